@@ -437,6 +437,179 @@ lh_status lh_distill(const float* A, const float* theta, const lh_c32* R, const 
                      int64_t D, int64_t d, int64_t L, float* loss, float* dA, float* dtheta,
                      lh_c32* dR, float* hhat, void* stream);
 
+/*
+ * The selective block: layer norm, a short causal convolution per channel and the
+ * selective state-space scan, the input-dependent sibling of the recurrence above,
+ * for prompts, single tokens and training.
+ *
+ * Rows: an input x [B, T, D] of these calls whose argument has an `ld` is read from
+ * rows of D consecutive elements, ld >= D elements apart: token t of batch row b is
+ * row b T + t (a slice of a projection's output needs no copy).  Outputs are
+ * contiguous.  Any element alignment is taken.  An output must not overlap any other
+ * buffer (a strided input is taken as the whole range from its first to its last
+ * element) but for the pairs named below, which may be the same buffer.
+ *
+ * lengths ([B] int32, or NULL): a right-padded batch; row b has lengths[b] tokens (a
+ * value outside [0, T] is taken as the nearer end).  Tokens past them are not read,
+ * their outputs and gradients are 0, and they leave the state alone.
+ *
+ * Sums, statistics and states are float32; bfloat16 outputs are rounded once, to
+ * nearest even.  Every call gives the same bits for the same inputs.  Sizes that need
+ * 2^32 threads or more in one launch return LH_ERR_INVALID_ARG.
+ */
+
+/*
+ * Layer norm over the last axis:
+ *   s = x (+ residual),  y = (s - mean s) / sqrt(var s + eps) * w + b
+ *
+ *   x, residual : [rows, D] (io_dtype); residual may be NULL
+ *   w, b        : [D] float32; b may be NULL
+ *   rows >= 0, D >= 1, eps >= 0
+ *   y           : out [rows, D] (io_dtype)
+ *   total       : out [rows, D] (io_dtype), s rounded; NULL, or with a residual (it may
+ *                 be the buffer of x or of residual).  y is formed from s unrounded.
+ *   mean, rstd  : out [rows] float32, mean s and 1 / sqrt(var s + eps), which the
+ *                 gradient takes; NULL where not needed
+ * One kernel launch; no workspace; same execution and error rules as lh_step.
+ */
+lh_status lh_layer_norm(const void* x, const void* residual, const float* w, const float* b,
+                        int64_t rows, int64_t D, float eps, lh_dtype io_dtype, void* y,
+                        void* total, float* mean, float* rstd, void* stream);
+
+/* Workspace bytes of lh_layer_norm_backward; (size_t)-1 for invalid sizes. */
+size_t lh_layer_norm_backward_workspace_bytes(int64_t rows, int64_t D);
+
+/*
+ * Gradients of lh_layer_norm, from what went in (x is s, the total where there was a
+ * residual) and its mean and rstd:
+ *   h = (x - mean) rstd,  g = dy w
+ *   dx = rstd (g - mean g - h mean(g h)) (+ dtotal),  dw = sum dy h,  db = sum dy
+ *
+ *   dy, x, dtotal : [rows, D] (io_dtype); dtotal, the gradient of total, may be NULL
+ *   dx            : out [rows, D] (io_dtype), of x and of residual alike; it may be the
+ *                   buffer of dtotal
+ *   dw, db        : out [D] float32; db may be NULL
+ *   workspace     : lh_layer_norm_backward_workspace_bytes bytes, 256-byte aligned (NULL
+ *                   allowed when that is 0)
+ */
+lh_status lh_layer_norm_backward(const void* dy, const void* x, const float* w, const float* mean,
+                                 const float* rstd, const void* dtotal, int64_t rows, int64_t D,
+                                 lh_dtype io_dtype, void* dx, float* dw, float* db,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Largest number of taps of the short convolution. */
+#define LH_SHORT_CONV_MAX_TAPS 8
+
+/*
+ * Short causal convolution, one filter of K taps per channel:
+ *   o_t = bias + sum_k w[c, k] x_(t - K + 1 + k),   y_t = silu ? o_t sigmoid(o_t) : o_t
+ * (w[c, K - 1] meets the current token).
+ *
+ *   x       : [B, T, D] (io_dtype), rows ld_x apart
+ *   w, bias : [D, K] and [D] float32; bias may be NULL
+ *   lengths : [B] int32 or NULL
+ *   B >= 1, T >= 0, D >= 1, 1 <= K <= LH_SHORT_CONV_MAX_TAPS
+ *   resume  : the inputs before the first token are the state's (else zeros, and the
+ *             state is not read)
+ *   state   : in/out [B, K - 1, D] (io_dtype): the last K - 1 inputs, oldest first
+ *             (NULL allowed when K = 1)
+ *   y       : out [B, T, D] (io_dtype)
+ * One kernel launch; no workspace.
+ */
+lh_status lh_short_conv_prefill(const void* x, int64_t ld_x, const float* w, const float* bias,
+                                const int32_t* lengths, int64_t B, int64_t T, int64_t D, int64_t K,
+                                lh_dtype io_dtype, int silu, int resume, void* state, void* y,
+                                void* stream);
+
+/* One token per batch row, x_t and y_t [B, D], the state in place: the outputs of a
+ * prefill that resumes with T = 1. */
+lh_status lh_short_conv_step(const void* x_t, int64_t ld_x, const float* w, const float* bias,
+                             int64_t B, int64_t D, int64_t K, lh_dtype io_dtype, int silu,
+                             void* state, void* y_t, void* stream);
+
+/* Workspace bytes of lh_short_conv_backward; (size_t)-1 for invalid sizes. */
+size_t lh_short_conv_backward_workspace_bytes(int64_t B, int64_t T, int64_t D, int64_t K);
+
+/*
+ * Gradients of lh_short_conv_prefill without resume: dx [B, T, D] (io_dtype), dw [D, K]
+ * and dbias [D] float32 (dbias may be NULL) from dy [B, T, D] (io_dtype) and the inputs.
+ * workspace as in lh_layer_norm_backward.
+ */
+lh_status lh_short_conv_backward(const void* dy, const void* x, int64_t ld_x, const float* w,
+                                 const float* bias, const int32_t* lengths, int64_t B, int64_t T,
+                                 int64_t D, int64_t K, lh_dtype io_dtype, int silu, void* dx,
+                                 float* dw, float* dbias, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/* Largest number of states per channel of the selective scan. */
+#define LH_SELECTIVE_MAX_STATES 128
+
+/*
+ * Selective state-space scan.  Per batch row, channel c and state n, g = c / (D / G):
+ *
+ *   delta = log(1 + exp(dt[b,t,c] + dt_bias[c]))
+ *   x[n]  = exp(delta A[c,n]) x[n] + delta Bm[b,t,g,n] u[b,t,c]
+ *   y     = sum_n Cm[b,t,g,n] x[n] + h0[c] u[b,t,c],  times z sigmoid(z) where z is given
+ *
+ * (the output reads the state after the update, unlike lh_step's.)
+ */
+typedef struct lh_selective_inputs {
+    const float* A;         /* [D, N] */
+    const float* dt_bias;   /* [D] or NULL (0) */
+    const float* h0;        /* [D] or NULL (0) */
+    const void* dt;         /* [B, T, D] (io_dtype), rows ld_dt apart */
+    const void* u;          /* [B, T, D] (io_dtype), rows ld_u apart */
+    const void* z;          /* [B, T, D] (io_dtype), rows ld_z apart; NULL: no gate */
+    const void* Bm;         /* [B, T, G, N] (io_dtype), rows of G N elements ld_B apart */
+    const void* Cm;         /* [B, T, G, N] (io_dtype), rows of G N elements ld_C apart */
+    const int32_t* lengths; /* [B] or NULL */
+    int64_t ld_dt, ld_u, ld_z, ld_B, ld_C;
+    int64_t B, T, D, N, G;  /* B >= 1, T >= 0, D >= 1, 1 <= N <= LH_SELECTIVE_MAX_STATES,
+                               G >= 1 divides D */
+    lh_dtype io_dtype;
+} lh_selective_inputs;
+
+/* Workspace bytes of lh_selective_prefill; (size_t)-1 for invalid sizes. */
+size_t lh_selective_workspace_bytes(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G);
+
+/*
+ * The scan over a prompt.
+ *   resume    : start from the state (else from zero, and the state is not read)
+ *   state     : in/out [B, D, N] float32, after each row's last token
+ *   y         : out [B, T, D] (io_dtype)
+ *   workspace : lh_selective_workspace_bytes bytes, 256-byte aligned (NULL allowed when
+ *               that is 0)
+ * One kernel launch, or three where the prompt is cut into chunks.
+ */
+lh_status lh_selective_prefill(const lh_selective_inputs* in, int resume, float* state, void* y,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token per batch row (T = 1, lengths NULL): y_t [B, D] and the state in place.  One
+ * kernel launch; no workspace. */
+lh_status lh_selective_step(const lh_selective_inputs* in, float* state, void* y_t, void* stream);
+
+/* What lh_selective_backward takes and gives beside the inputs. */
+typedef struct lh_selective_grads {
+    const void* dy;  /* [B, T, D] (io_dtype): the gradient of y */
+    void* ddt;       /* out [B, T, D] (io_dtype) */
+    void* du;        /* out [B, T, D] (io_dtype) */
+    void* dz;        /* out [B, T, D] (io_dtype); NULL where z is NULL, and only there */
+    void* dBm;       /* out [B, T, G, N] (io_dtype) */
+    void* dCm;       /* out [B, T, G, N] (io_dtype) */
+    float* dA;       /* out [D, N] */
+    float* dh0;      /* out [D], or NULL */
+    float* ddt_bias; /* out [D], or NULL */
+} lh_selective_grads;
+
+/* Workspace bytes of lh_selective_backward; (size_t)-1 for invalid sizes. */
+size_t lh_selective_backward_workspace_bytes(int64_t B, int64_t T, int64_t D, int64_t N,
+                                             int64_t G);
+
+/* Gradients of lh_selective_prefill without resume, from its inputs alone (the states
+ * are formed again).  workspace as there. */
+lh_status lh_selective_backward(const lh_selective_inputs* in, const lh_selective_grads* grads,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -12,6 +12,12 @@ kernels; there is no fallback.  PyTorch provides device memory and streams.
     prefill_fft(lam, R, h0, u, state, y)  # the same results by FFT convolution
     step(lam, R, h0, state, u_t, y_t)  # y_t from x_t, then x_{t+1} in place
 
+The selective block beside it (prompts, single tokens, gradients):
+
+    layer_norm, layer_norm_backward
+    short_conv_prefill, short_conv_step, short_conv_backward
+    selective_prefill, selective_step, selective_backward
+
 ``lam``, ``R``: complex64 ``[D, d]``; ``h0``: float32 ``[D]``; ``u``, ``y``:
 float32 or bfloat16 ``[B, T, D]``; ``state``: complex64 ``[B, D, d]``;
 ``u_t``, ``y_t``: ``[B, D]``.
@@ -48,6 +54,18 @@ __all__ = [
     "companion_step",
     "companion_init_workspace_bytes",
     "companion_init",
+    "layer_norm",
+    "layer_norm_backward_workspace_bytes",
+    "layer_norm_backward",
+    "short_conv_prefill",
+    "short_conv_step",
+    "short_conv_backward_workspace_bytes",
+    "short_conv_backward",
+    "selective_workspace_bytes",
+    "selective_prefill",
+    "selective_step",
+    "selective_backward_workspace_bytes",
+    "selective_backward",
     "STATUS",
 ]
 
@@ -76,6 +94,16 @@ _lib: Optional[ctypes.CDLL] = None
 # torch and its current-stream lookup, set when the library is loaded
 _torch = None
 _raw_stream = None
+
+
+class _SelectiveInputs(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("A", "dt_bias", "h0", "dt", "u", "z", "Bm", "Cm", "lengths")]
+                + [(k, ctypes.c_int64) for k in ("ld_dt", "ld_u", "ld_z", "ld_B", "ld_C", "B", "T", "D", "N", "G")]
+                + [("io_dtype", ctypes.c_int)])
+
+
+class _SelectiveGrads(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("dy", "ddt", "du", "dz", "dBm", "dCm", "dA", "dh0", "ddt_bias")]
 
 
 class LHError(RuntimeError):
@@ -149,6 +177,30 @@ def lib() -> ctypes.CDLL:
     L.lh_companion_init_workspace_bytes.restype = sz
     L.lh_companion_init.argtypes = [vp, vp, i64, i64, i64, i64, ctypes.c_int, vp, vp, sz, vp]
     L.lh_companion_init.restype = ctypes.c_int
+    ci, cf = ctypes.c_int, ctypes.c_float
+    L.lh_layer_norm.argtypes = [vp, vp, vp, vp, i64, i64, cf, ci, vp, vp, vp, vp, vp]
+    L.lh_layer_norm.restype = ci
+    L.lh_layer_norm_backward_workspace_bytes.argtypes = [i64, i64]
+    L.lh_layer_norm_backward_workspace_bytes.restype = sz
+    L.lh_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, ci, vp, vp, vp, vp, sz, vp]
+    L.lh_layer_norm_backward.restype = ci
+    L.lh_short_conv_prefill.argtypes = [vp, i64, vp, vp, vp, i64, i64, i64, i64, ci, ci, ci, vp, vp, vp]
+    L.lh_short_conv_prefill.restype = ci
+    L.lh_short_conv_step.argtypes = [vp, i64, vp, vp, i64, i64, i64, ci, ci, vp, vp, vp]
+    L.lh_short_conv_step.restype = ci
+    L.lh_short_conv_backward_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    L.lh_short_conv_backward_workspace_bytes.restype = sz
+    L.lh_short_conv_backward.argtypes = [vp, vp, i64, vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, vp, vp, vp, sz, vp]
+    L.lh_short_conv_backward.restype = ci
+    for name in ("lh_selective_workspace_bytes", "lh_selective_backward_workspace_bytes"):
+        getattr(L, name).argtypes = [i64, i64, i64, i64, i64]
+        getattr(L, name).restype = sz
+    L.lh_selective_prefill.argtypes = [vp, ci, vp, vp, vp, sz, vp]
+    L.lh_selective_prefill.restype = ci
+    L.lh_selective_step.argtypes = [vp, vp, vp, vp]
+    L.lh_selective_step.restype = ci
+    L.lh_selective_backward.argtypes = [vp, vp, vp, sz, vp]
+    L.lh_selective_backward.restype = ci
     _lib = L
     return L
 
@@ -445,3 +497,260 @@ def companion_init(a, u, state, workspace=None, stream=None) -> None:
                                          u.device, stream)
     _check(lib().lh_companion_init(a.data_ptr(), u.data_ptr(), B, D, order // 2, T, _io_dtype(u),
                                    state.data_ptr(), ws_ptr, ws_len, handle))
+
+
+# ---- the selective block
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _need_rows(t, name, dtype, lead, row) -> int:
+    """Checks ``t`` of shape ``lead + row`` (``lead``: ``(B, T)`` or ``(B,)``): contiguous
+    rows, a fixed distance apart; returns that distance in elements."""
+    if not isinstance(t, _torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a HIP device, got {t.device}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != lead + row:
+        raise ValueError(f"{name} must have shape {lead + row}, got {tuple(t.shape)}")
+    strides, width = t.stride(), 1
+    for n, s in zip(row[::-1], strides[::-1]):
+        if n > 1 and s != width:
+            raise ValueError(f"{name} must have contiguous rows")
+        width *= n
+    # (the stride of an axis of one says nothing)
+    if len(lead) == 1 or lead[1] == 1:
+        ld = strides[0] if lead[0] > 1 else width
+    else:
+        ld = strides[1]
+        if lead[0] > 1 and lead[1] > 0 and strides[0] != lead[1] * ld:
+            raise ValueError(f"{name}: the rows of its batches must follow one another")
+    if t.numel() == 0:
+        return width
+    if ld < width:
+        raise ValueError(f"{name} must have rows that do not overlap")
+    return ld
+
+
+def _need_lengths(lengths, B):
+    if lengths is not None:
+        _need(lengths, "lengths", _torch.int32, (B,))
+
+
+def _block_bytes(name, *sizes) -> int:
+    n = getattr(lib(), name)(*sizes)
+    if n == ctypes.c_size_t(-1).value:
+        raise LHError(1, lib().lh_last_error().decode(errors="replace"))
+    return int(n)
+
+
+def layer_norm(x, w, b, y, residual=None, total=None, mean=None, rstd=None, eps: float = 1e-5,
+               stream=None) -> None:
+    """Layer norm over the last axis of ``x`` (``lh_layer_norm``), of ``x + residual``
+    where a residual is given; ``total`` receives that sum (it may be ``x`` or
+    ``residual`` itself).  ``mean``, ``rstd``: float32, one per row, for the gradient.
+    ``w``, ``b``: float32 ``[D]`` (``b`` may be None)."""
+    torch = _torch_loaded()
+    shape, D = x.shape, x.shape[-1]
+    rows = x.numel() // D if D else 0
+    _need(x, "x", x.dtype, shape)
+    _need(w, "w", torch.float32, (D,))
+    if b is not None:
+        _need(b, "b", torch.float32, (D,))
+    _need(y, "y", x.dtype, shape)
+    for name, t in (("residual", residual), ("total", total)):
+        if t is not None:
+            _need(t, name, x.dtype, shape)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t is not None:
+            _need(t, name, torch.float32, shape[:-1])
+    _check(lib().lh_layer_norm(x.data_ptr(), _ptr(residual), w.data_ptr(), _ptr(b), rows, D, eps,
+                               _io_dtype(x), y.data_ptr(), _ptr(total), _ptr(mean), _ptr(rstd),
+                               _handle(x, stream)))
+
+
+def layer_norm_backward_workspace_bytes(rows: int, D: int) -> int:
+    return _block_bytes("lh_layer_norm_backward_workspace_bytes", rows, D)
+
+
+def layer_norm_backward(dy, x, w, mean, rstd, dx, dw, db=None, dtotal=None, workspace=None,
+                        stream=None) -> None:
+    """Gradients of ``layer_norm`` (``lh_layer_norm_backward``): ``x`` is what was
+    normalised (the total), ``dtotal`` the gradient that reaches it from elsewhere,
+    which is added to ``dx`` (and may be ``dx`` itself)."""
+    torch = _torch_loaded()
+    shape, D = x.shape, x.shape[-1]
+    rows = x.numel() // D if D else 0
+    _need(x, "x", x.dtype, shape)
+    _need(dy, "dy", x.dtype, shape)
+    _need(dx, "dx", x.dtype, shape)
+    if dtotal is not None:
+        _need(dtotal, "dtotal", x.dtype, shape)
+    _need(w, "w", torch.float32, (D,))
+    _need(dw, "dw", torch.float32, (D,))
+    if db is not None:
+        _need(db, "db", torch.float32, (D,))
+    _need(mean, "mean", torch.float32, shape[:-1])
+    _need(rstd, "rstd", torch.float32, shape[:-1])
+    handle = _handle(x, stream)
+    workspace, ws_ptr, ws_len = _scratch(layer_norm_backward_workspace_bytes(rows, D), workspace,
+                                         x.device, stream)
+    _check(lib().lh_layer_norm_backward(dy.data_ptr(), x.data_ptr(), w.data_ptr(), mean.data_ptr(),
+                                        rstd.data_ptr(), _ptr(dtotal), rows, D, _io_dtype(x),
+                                        dx.data_ptr(), dw.data_ptr(), _ptr(db), ws_ptr, ws_len,
+                                        handle))
+
+
+def _conv_args(x, w, bias, lead):
+    torch = _torch_loaded()
+    D, K = w.shape
+    ld = _need_rows(x, "x", x.dtype, lead, (D,))
+    _need(w, "w", torch.float32, (D, K))
+    if bias is not None:
+        _need(bias, "bias", torch.float32, (D,))
+    return ld, D, K, _io_dtype(x)
+
+
+def short_conv_prefill(x, w, bias, state, y, silu: bool = True, lengths=None, resume: bool = False,
+                       stream=None) -> None:
+    """Short causal convolution of the prompt ``x [B, T, D]`` with the taps ``w [D, K]``
+    (``lh_short_conv_prefill``); ``state [B, K - 1, D]`` receives the last inputs, and is
+    what the prompt continues from where ``resume``.  ``x`` may be a slice of rows."""
+    B, T = x.shape[:2]
+    ld, D, K, io = _conv_args(x, w, bias, (B, T))
+    _need(state, "state", x.dtype, (B, K - 1, D))
+    _need(y, "y", x.dtype, (B, T, D))
+    _need_lengths(lengths, B)
+    _check(lib().lh_short_conv_prefill(x.data_ptr(), ld, w.data_ptr(), _ptr(bias), _ptr(lengths), B,
+                                       T, D, K, io, silu, resume, state.data_ptr(), y.data_ptr(),
+                                       _handle(x, stream)))
+
+
+def short_conv_step(x_t, w, bias, state, y_t, silu: bool = True, stream=None) -> None:
+    """One token per row, ``x_t``, ``y_t`` ``[B, D]``, ``state`` in place
+    (``lh_short_conv_step``)."""
+    B = x_t.shape[0]
+    ld, D, K, io = _conv_args(x_t, w, bias, (B,))
+    _need(state, "state", x_t.dtype, (B, K - 1, D))
+    _need(y_t, "y_t", x_t.dtype, (B, D))
+    _check(lib().lh_short_conv_step(x_t.data_ptr(), ld, w.data_ptr(), _ptr(bias), B, D, K, io, silu,
+                                    state.data_ptr(), y_t.data_ptr(), _handle(x_t, stream)))
+
+
+def short_conv_backward_workspace_bytes(B: int, T: int, D: int, K: int) -> int:
+    return _block_bytes("lh_short_conv_backward_workspace_bytes", B, T, D, K)
+
+
+def short_conv_backward(dy, x, w, bias, dx, dw, dbias=None, silu: bool = True, lengths=None,
+                        workspace=None, stream=None) -> None:
+    """Gradients of ``short_conv_prefill`` from zero inputs before the prompt
+    (``lh_short_conv_backward``)."""
+    torch = _torch_loaded()
+    B, T = x.shape[:2]
+    ld, D, K, io = _conv_args(x, w, bias, (B, T))
+    _need(dy, "dy", x.dtype, (B, T, D))
+    _need(dx, "dx", x.dtype, (B, T, D))
+    _need(dw, "dw", torch.float32, (D, K))
+    if dbias is not None:
+        _need(dbias, "dbias", torch.float32, (D,))
+    _need_lengths(lengths, B)
+    handle = _handle(x, stream)
+    workspace, ws_ptr, ws_len = _scratch(short_conv_backward_workspace_bytes(B, T, D, K), workspace,
+                                         x.device, stream)
+    _check(lib().lh_short_conv_backward(dy.data_ptr(), x.data_ptr(), ld, w.data_ptr(), _ptr(bias),
+                                        _ptr(lengths), B, T, D, K, io, silu, dx.data_ptr(),
+                                        dw.data_ptr(), _ptr(dbias), ws_ptr, ws_len, handle))
+
+
+def _selective_args(A, dt, Bm, Cm, u, h0, dt_bias, z, lengths, lead, suffix=""):
+    torch = _torch_loaded()
+    D, N = A.shape
+    G = Bm.shape[-2]
+    s = _SelectiveInputs()
+    _need(A, "A", torch.float32, (D, N))
+    for name, t in (("dt_bias", dt_bias), ("h0", h0)):
+        if t is not None:
+            _need(t, name, torch.float32, (D,))
+            setattr(s, name, t.data_ptr())
+    dtype = u.dtype
+    s.io_dtype = _io_dtype(u)
+    s.A = A.data_ptr()
+    s.ld_dt = _need_rows(dt, "dt" + suffix, dtype, lead, (D,))
+    s.ld_u = _need_rows(u, "u" + suffix, dtype, lead, (D,))
+    s.ld_B = _need_rows(Bm, "Bm" + suffix, dtype, lead, (G, N))
+    s.ld_C = _need_rows(Cm, "Cm" + suffix, dtype, lead, (G, N))
+    s.dt, s.u, s.Bm, s.Cm = dt.data_ptr(), u.data_ptr(), Bm.data_ptr(), Cm.data_ptr()
+    if z is not None:
+        s.ld_z = _need_rows(z, "z", dtype, lead, (D,))
+        s.z = z.data_ptr()
+    if lengths is not None:
+        _need_lengths(lengths, lead[0])
+        s.lengths = lengths.data_ptr()
+    s.B, s.T, s.D, s.N, s.G = lead[0], lead[1] if len(lead) > 1 else 1, D, N, G
+    return s
+
+
+def selective_workspace_bytes(B: int, T: int, D: int, N: int, G: int = 1) -> int:
+    return _block_bytes("lh_selective_workspace_bytes", B, T, D, N, G)
+
+
+def selective_prefill(A, dt, Bm, Cm, u, state, y, h0=None, dt_bias=None, z=None, lengths=None,
+                      resume: bool = False, workspace=None, stream=None) -> None:
+    """Selective scan of a prompt (``lh_selective_prefill``): ``dt``, ``u``, ``z``
+    ``[B, T, D]``, ``Bm``, ``Cm`` ``[B, T, G, N]`` (all may be slices of rows), ``A [D, N]``,
+    ``h0``, ``dt_bias`` ``[D]`` and ``state [B, D, N]`` float32; writes ``y [B, T, D]`` and the
+    state, which the prompt continues from where ``resume``."""
+    B, T = u.shape[:2]
+    s = _selective_args(A, dt, Bm, Cm, u, h0, dt_bias, z, lengths, (B, T))
+    _need(state, "state", _torch.float32, (B, s.D, s.N))
+    _need(y, "y", u.dtype, (B, T, s.D))
+    handle = _handle(u, stream)
+    workspace, ws_ptr, ws_len = _scratch(selective_workspace_bytes(B, T, s.D, s.N, s.G), workspace,
+                                         u.device, stream)
+    _check(lib().lh_selective_prefill(ctypes.byref(s), resume, state.data_ptr(), y.data_ptr(), ws_ptr,
+                                      ws_len, handle))
+
+
+def selective_step(A, dt_t, Bm_t, Cm_t, u_t, state, y_t, h0=None, dt_bias=None, z=None,
+                   stream=None) -> None:
+    """One token per row (``lh_selective_step``): ``dt_t``, ``u_t``, ``z`` ``[B, D]``,
+    ``Bm_t``, ``Cm_t`` ``[B, G, N]``, ``state`` in place."""
+    B = u_t.shape[0]
+    s = _selective_args(A, dt_t, Bm_t, Cm_t, u_t, h0, dt_bias, z, None, (B,), "_t")
+    _need(state, "state", _torch.float32, (B, s.D, s.N))
+    _need(y_t, "y_t", u_t.dtype, (B, s.D))
+    _check(lib().lh_selective_step(ctypes.byref(s), state.data_ptr(), y_t.data_ptr(),
+                                   _handle(u_t, stream)))
+
+
+def selective_backward_workspace_bytes(B: int, T: int, D: int, N: int, G: int = 1) -> int:
+    return _block_bytes("lh_selective_backward_workspace_bytes", B, T, D, N, G)
+
+
+def selective_backward(dy, A, dt, Bm, Cm, u, dA, ddt, dBm, dCm, du, h0=None, dh0=None, dt_bias=None,
+                       ddt_bias=None, z=None, dz=None, lengths=None, workspace=None,
+                       stream=None) -> None:
+    """Gradients of ``selective_prefill`` from a zero state (``lh_selective_backward``),
+    from its inputs and ``dy [B, T, D]``."""
+    torch = _torch_loaded()
+    B, T = u.shape[:2]
+    s = _selective_args(A, dt, Bm, Cm, u, h0, dt_bias, z, lengths, (B, T))
+    D, N, G = s.D, s.N, s.G
+    g = _SelectiveGrads()
+    for name, t, dtype, shape in (
+            ("dy", dy, u.dtype, (B, T, D)), ("ddt", ddt, u.dtype, (B, T, D)), ("du", du, u.dtype, (B, T, D)),
+            ("dz", dz, u.dtype, (B, T, D)), ("dBm", dBm, u.dtype, (B, T, G, N)),
+            ("dCm", dCm, u.dtype, (B, T, G, N)), ("dA", dA, torch.float32, (D, N)),
+            ("dh0", dh0, torch.float32, (D,)), ("ddt_bias", ddt_bias, torch.float32, (D,))):
+        if t is not None:
+            _need(t, name, dtype, shape)
+            setattr(g, name, t.data_ptr())
+        elif name not in ("dz", "dh0", "ddt_bias"):
+            raise TypeError(f"{name} must be a torch.Tensor")
+    handle = _handle(u, stream)
+    workspace, ws_ptr, ws_len = _scratch(selective_backward_workspace_bytes(B, T, D, N, G), workspace,
+                                         u.device, stream)
+    _check(lib().lh_selective_backward(ctypes.byref(s), ctypes.byref(g), ws_ptr, ws_len, handle))

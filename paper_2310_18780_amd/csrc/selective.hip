@@ -1,0 +1,352 @@
+// The selective state-space scan, for prompts and for single tokens:
+//
+//   delta = softplus(dt + dt_bias)
+//   x_t[n] = e^(delta A[n]) x_(t-1)[n] + delta B_t[n] u_t
+//   y_t = sum_n C_t[n] x_t[n] + h0 u_t,  times silu(z_t) where there is a gate
+//
+// per batch row and channel, B and C shared by the channels of a group.
+//
+// Prompts.  A lane is a channel, so u, dt, z and y are read and written in whole
+// lines, once.  The states of a 64-channel tile are split over the wavefronts of a
+// workgroup, ns to a lane in registers; a tile of 16 steps passes through LDS: its
+// wavefronts form the steps (delta, delta u) of some rows each, walk all 16 rows for
+// their own states, and add the wavefronts' parts of y for some rows each.  Per state
+// and step that is two products, two multiply-adds and an exponential; the
+// exponential (8 cycles) and the four (4 cycles each) are what bounds the kernel.
+//
+// Where batch rows and tiles leave SIMDs idle the prompt is cut into chunks: a first
+// pass forms each chunk's end state from zero and its sum of steps (a chunk's decay is
+// e^(A sum delta), one exponential), a carry turns end states into entry states, and
+// the output pass starts every chunk from its own.
+//
+// Single tokens: four states of a (batch row, channel) to a lane, y summed over the
+// row's lanes; bound by the state, read once and written once.
+#include "selective.hpp"
+
+namespace lh {
+namespace {
+
+constexpr int kSteps = 16;  // steps of a tile
+
+template <typename T, int NS, int S, bool OUT>
+__global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chunk,
+                                                        int64_t nchunks, float* xs, float* sums,
+                                                        float* state, bool resume, T* y)
+{
+    constexpr int R = kSteps / S;    // rows per wavefront
+    constexpr int W = OUT ? 2 : 1;   // B (and C)
+    constexpr int E = kSteps * S * W * NS;
+    constexpr int PER = (E + kWave * S - 1) / (kWave * S);
+    __shared__ float2 step[kSteps][kWave];                    // delta, delta u
+    __shared__ __align__(16) float rows[kSteps][S][W][NS];    // B, C
+    __shared__ float part[OUT ? S : 1][kSteps][kWave];        // the wavefronts' parts of y
+
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int N = s.N;
+    const int64_t Dg = s.D / s.G, per = group_tiles(s.D, s.G), tiles = per * s.G;
+    const int64_t tile = blockIdx.x % tiles, rest = blockIdx.x / tiles;
+    const int64_t k = rest % nchunks, b = rest / nchunks;
+    const int64_t grp = tile / per, cg = (tile % per) * kWave + lane;
+    const bool own = cg < Dg;  // lanes past the group compute its last channel and store nothing
+    const int64_t c = grp * Dg + (own ? cg : Dg - 1);
+    const int n0 = wave * NS, real = N - n0 < NS ? N - n0 : NS;
+
+    const int64_t len = tokens_of(s.lengths, b, s.T);
+    const int64_t t_begin = k * chunk, t_end = t_begin + chunk < s.T ? t_begin + chunk : s.T;
+    const int64_t te = t_end < len ? t_end : len;
+
+    const T* pu = static_cast<const T*>(s.u) + b * s.T * s.ld_u + c;
+    const T* pdt = static_cast<const T*>(s.dt) + b * s.T * s.ld_dt + c;
+    const T* pz = OUT && s.z ? static_cast<const T*>(s.z) + b * s.T * s.ld_z + c : nullptr;
+    const T* pB = static_cast<const T*>(s.Bm) + b * s.T * s.ld_b + grp * N;
+    const T* pC = static_cast<const T*>(s.Cm) + b * s.T * s.ld_c + grp * N;
+    const float bias = s.dt_bias ? s.dt_bias[c] : 0.f;
+    const float h0 = OUT && s.h0 ? s.h0[c] : 0.f;
+
+    float A2[NS], x[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        A2[i] = i < real ? s.A[c * N + n0 + i] * kLog2e : 0.f;
+        x[i] = 0.f;
+        if (OUT && i < real) {
+            if (nchunks > 1)
+                x[i] = xs[((b * nchunks + k) * N + n0 + i) * s.D + c];
+            else if (resume)
+                x[i] = state[(b * s.D + c) * N + n0 + i];
+        }
+    }
+    float total = 0.f;  // sum of the steps
+
+    float du[R], dd[R], dz[R], dr[PER];  // the next tile's values in flight
+    auto load = [&](int64_t t0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t t = t0 + wave * R + r;
+            du[r] = dd[r] = dz[r] = 0.f;
+            if (t < te) {
+                du[r] = io_load(pu + t * s.ld_u);
+                dd[r] = io_load(pdt + t * s.ld_dt);
+                if (OUT && pz) dz[r] = io_load(pz + t * s.ld_z);
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int e = threadIdx.x + p * kWave * S;
+            const int j = e / (S * W * NS), f = e % (S * W * NS);
+            const int n = f / (W * NS) * NS + f % NS, which = f / NS % W;
+            dr[p] = 0.f;
+            if (e < E && t0 + j < te && n < N)
+                dr[p] = which ? io_load(pC + (t0 + j) * s.ld_c + n) : io_load(pB + (t0 + j) * s.ld_b + n);
+        }
+    };
+    load(t_begin);
+    for (int64_t t0 = t_begin; t0 < te; t0 += kSteps) {
+        float cu[R], cz[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int j = wave * R + r;
+            // a step past the row's end is 0: the state stays
+            const float delta = t0 + j < te ? softplus(dd[r] + bias) : 0.f;
+            cu[r] = du[r];
+            cz[r] = dz[r];
+            step[j][lane] = make_float2(delta, delta * du[r]);
+        }
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int e = threadIdx.x + p * kWave * S;
+            if (e < E) (&rows[0][0][0][0])[e] = dr[p];
+        }
+        __syncthreads();
+        load(t0 + kSteps);
+#pragma unroll 4
+        for (int j = 0; j < kSteps; ++j) {
+            const float2 d = step[j][lane];
+            float acc = 0.f;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                const float a = exp2_fast(d.x * A2[i]);
+                x[i] = fmaf(a, x[i], d.y * rows[j][wave][0][i]);
+                // (slots past N take no part: 0 times an infinite input is not 0)
+                if constexpr (OUT) acc = i < real ? fmaf(rows[j][wave][W - 1][i], x[i], acc) : acc;
+            }
+            if constexpr (OUT)
+                part[wave][j][lane] = acc;
+            else
+                total += d.x;
+        }
+        __syncthreads();
+        if constexpr (OUT) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int j = wave * R + r;
+                float o = h0 * cu[r];
+#pragma unroll
+                for (int w = 0; w < S; ++w) o += part[w][j][lane];
+                if (pz) o *= cz[r] * sigmoid(cz[r]);
+                if (own && t0 + j < te) io_store(y + (b * s.T + t0 + j) * s.D + c, o);
+            }
+        }
+    }
+    if constexpr (OUT) {
+        for (int64_t t = (te > t_begin ? te : t_begin) + wave; t < t_end; t += S)
+            if (own) io_store(y + (b * s.T + t) * s.D + c, 0.f);
+        if (k == nchunks - 1 && own) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+                if (i < real) state[(b * s.D + c) * N + n0 + i] = x[i];
+        }
+    } else if (own) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+            if (i < real) xs[((b * nchunks + k) * N + n0 + i) * s.D + c] = x[i];
+        if (wave == 0) sums[(b * nchunks + k) * s.D + c] = total;
+    }
+}
+
+// End states from zero become entry states, in place.
+__global__ __launch_bounds__(256) void carry_kernel(const float* __restrict__ A,
+                                                    const float* __restrict__ sums,
+                                                    float* __restrict__ xs,
+                                                    const float* __restrict__ state, bool resume,
+                                                    int64_t B, int64_t D, int N, int64_t nchunks)
+{
+    const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t c = id % D, n = id / D % N, b = id / (D * N);
+    if (b >= B) return;
+    const float A2 = A[c * N + n] * kLog2e;
+    float* px = xs + (b * nchunks * N + n) * D + c;
+    const float* ps = sums + b * nchunks * D + c;
+    float x = resume ? state[(b * D + c) * N + n] : 0.f;
+    constexpr int U = 8;
+    for (int64_t k = 0; k < nchunks; k += U) {
+        float end[U], a[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (k + i < nchunks) {
+                end[i] = px[(k + i) * N * D];
+                a[i] = ps[(k + i) * D];
+            }
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (k + i < nchunks) {
+                px[(k + i) * N * D] = x;
+                x = fmaf(exp2_fast(A2 * a[i]), x, end[i]);
+            }
+    }
+}
+
+// Four states to a lane, LPR lanes to a (batch row, channel).
+template <typename T, int LPR>
+__global__ __launch_bounds__(256) void scan_step_kernel(Selective s, float* __restrict__ state,
+                                                        T* __restrict__ y)
+{
+    const int sub = threadIdx.x % LPR;
+    const int64_t row = (int64_t(blockIdx.x) * 256 + threadIdx.x) / LPR;
+    if (row >= s.B * s.D) return;
+    const int64_t b = row / s.D, c = row - b * s.D;
+    const int64_t grp = c / (s.D / s.G);
+    const int n = sub * 4, cnt = s.N - n;
+    float* px = state + row * s.N + n;
+    float x[4], A[4], Bv[4], Cv[4];
+    load_some<4>(px, cnt, x);
+    load_some<4>(s.A + c * s.N + n, cnt, A);
+    load_some<4>(static_cast<const T*>(s.Bm) + b * s.ld_b + grp * s.N + n, cnt, Bv);
+    load_some<4>(static_cast<const T*>(s.Cm) + b * s.ld_c + grp * s.N + n, cnt, Cv);
+    const float u = io_load(static_cast<const T*>(s.u) + b * s.ld_u + c);
+    const float delta = softplus(io_load(static_cast<const T*>(s.dt) + b * s.ld_dt + c) +
+                                 (s.dt_bias ? s.dt_bias[c] : 0.f));
+    const float du = delta * u;
+    float o = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = fmaf(exp2_fast(delta * (A[i] * kLog2e)), x[i], du * Bv[i]);
+        if (i < cnt) o = fmaf(Cv[i], x[i], o);
+    }
+    store_some<4>(px, cnt, x);
+#pragma unroll
+    for (int off = 1; off < LPR; off *= 2) o += __shfl_xor(o, off, kWave);
+    if (sub == 0) {
+        if (s.h0) o = fmaf(s.h0[c], u, o);
+        if (s.z) {
+            const float z = io_load(static_cast<const T*>(s.z) + b * s.ld_z + c);
+            o *= z * sigmoid(z);
+        }
+        io_store(y + row, o);
+    }
+}
+
+// States per lane and wavefronts per tile.
+void split_states(int N, int* ns, int* waves)
+{
+    *waves = N <= 16 ? 4 : N <= 32 ? 8 : 16;
+    *ns = (N + *waves - 1) / *waves;
+    if (*ns > 4) *ns = *ns <= 6 ? 6 : 8;
+}
+
+template <typename F>
+hipError_t with_split(int ns, int waves, F f)
+{
+#define LH_SPLIT(n, w) \
+    if (ns == n && waves == w) \
+    return f(std::integral_constant<int, n>(), std::integral_constant<int, w>())
+    LH_SPLIT(1, 4);
+    LH_SPLIT(2, 4);
+    LH_SPLIT(3, 4);
+    LH_SPLIT(4, 4);
+    LH_SPLIT(3, 8);
+    LH_SPLIT(4, 8);
+    LH_SPLIT(3, 16);
+    LH_SPLIT(4, 16);
+    LH_SPLIT(6, 16);
+    LH_SPLIT(8, 16);
+#undef LH_SPLIT
+    return hipErrorInvalidValue;
+}
+
+template <typename T>
+hipError_t scan(const Selective& s, float* state, bool resume, T* y, void* workspace,
+                hipStream_t stream)
+{
+    const SelectivePlan p = selective_plan(s.B, s.T, s.D, s.N, s.G);
+    const int64_t blocks = s.B * p.nchunks * group_tiles(s.D, s.G) * s.G;
+    float* xs = static_cast<float*>(workspace);
+    float* sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.off_sums);
+    return with_split(p.ns, p.waves, [&](auto ns, auto waves) {
+        constexpr int NS = decltype(ns)::value, S = decltype(waves)::value;
+        if (p.nchunks > 1) {
+            hipLaunchKernelGGL((scan_kernel<T, NS, S, false>), dim3(uint32_t(blocks)),
+                               dim3(kWave * S), 0, stream, s, p.chunk, p.nchunks, xs, sums, state,
+                               resume, y);
+            hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            hipLaunchKernelGGL(carry_kernel, dim3(uint32_t((s.B * s.D * s.N + 255) / 256)),
+                               dim3(256), 0, stream, s.A, sums, xs, state, resume, s.B, s.D, s.N,
+                               p.nchunks);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL((scan_kernel<T, NS, S, true>), dim3(uint32_t(blocks)), dim3(kWave * S),
+                           0, stream, s, p.chunk, p.nchunks, xs, sums, state, resume, y);
+        return hipGetLastError();
+    });
+}
+
+template <typename T>
+hipError_t scan_step(const Selective& s, float* state, T* y, hipStream_t stream)
+{
+    int lpr = 1;
+    while (lpr * 4 < s.N) lpr *= 2;
+    const dim3 grid(uint32_t((s.B * s.D * lpr + 255) / 256));
+    switch (lpr) {
+#define LH_STEP(l) \
+    case l: \
+        hipLaunchKernelGGL((scan_step_kernel<T, l>), grid, dim3(256), 0, stream, s, state, y); \
+        break
+        LH_STEP(1);
+        LH_STEP(2);
+        LH_STEP(4);
+        LH_STEP(8);
+        LH_STEP(16);
+        default:
+            LH_STEP(32);
+#undef LH_STEP
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+SelectivePlan selective_plan(int64_t B, int64_t T, int64_t D, int N, int G)
+{
+    SelectivePlan p;
+    split_states(N, &p.ns, &p.waves);
+    const int64_t waves = B * group_tiles(D, G) * G * p.waves;
+    // two wavefronts per SIMD, chunks of 32 steps or more
+    int64_t n = waves >= 1024 ? 1 : (2048 + waves - 1) / waves;
+    if (n > T / 32) n = T / 32;
+    if (n < 3) n = 1;
+    p.chunk = ((T + n - 1) / n + kSteps - 1) / kSteps * kSteps;
+    if (p.chunk < kSteps) p.chunk = kSteps;
+    p.nchunks = T > 0 ? (T + p.chunk - 1) / p.chunk : 1;
+    p.off_sums = p.ws_bytes = 0;
+    if (p.nchunks > 1) {
+        p.off_sums = size_t(B) * p.nchunks * N * D * sizeof(float);
+        p.ws_bytes = p.off_sums + size_t(B) * p.nchunks * D * sizeof(float);
+    }
+    return p;
+}
+
+hipError_t launch_selective(const Selective& s, float* state, bool resume, void* y,
+                            void* workspace, hipStream_t stream)
+{
+    return s.bf16_io ? scan(s, state, resume, static_cast<bf16*>(y), workspace, stream)
+                     : scan(s, state, resume, static_cast<float*>(y), workspace, stream);
+}
+
+hipError_t launch_selective_step(const Selective& s, float* state, void* y, hipStream_t stream)
+{
+    return s.bf16_io ? scan_step(s, state, static_cast<bf16*>(y), stream)
+                     : scan_step(s, state, static_cast<float*>(y), stream);
+}
+
+}  // namespace lh
