@@ -28,6 +28,20 @@ namespace {
 
 constexpr int kSteps = 16;  // steps of a tile
 
+// f with n as a constant, 0 <= n <= MOST (n < 0 is 0).
+template <int MOST, typename F>
+__device__ __forceinline__ void with_count(int n, F& f)
+{
+    if constexpr (MOST <= 0) {
+        f(std::integral_constant<int, 0>());
+    } else {
+        if (n == MOST)
+            f(std::integral_constant<int, MOST>());
+        else
+            with_count<MOST - 1>(n, f);
+    }
+}
+
 template <typename T, int NS, int S, bool OUT>
 __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chunk,
                                                         int64_t nchunks, float* xs, float* sums,
@@ -47,20 +61,25 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     const int64_t Dg = s.D / s.G, per = group_tiles(s.D, s.G), tiles = per * s.G;
     const int64_t tile = blockIdx.x % tiles, rest = blockIdx.x / tiles;
     const int64_t k = rest % nchunks, b = rest / nchunks;
-    const int64_t grp = tile / per, cg = (tile % per) * kWave + lane;
-    const bool own = cg < Dg;  // lanes past the group compute its last channel and store nothing
-    const int64_t c = grp * Dg + (own ? cg : Dg - 1);
+    const int64_t grp = tile / per, c0 = grp * Dg + (tile % per) * kWave;  // the tile's first channel
+    const int width = int((grp + 1) * Dg - c0 < kWave ? (grp + 1) * Dg - c0 : kWave);
+    const bool own = lane < width;  // lanes past the group compute its last channel and store nothing
+    const uint32_t lc = own ? lane : width - 1;
     const int n0 = wave * NS, real = N - n0 < NS ? N - n0 : NS;
 
     const int64_t len = tokens_of(s.lengths, b, s.T);
     const int64_t t_begin = k * chunk, t_end = t_begin + chunk < s.T ? t_begin + chunk : s.T;
     const int64_t te = t_end < len ? t_end : len;
 
-    const T* pu = static_cast<const T*>(s.u) + b * s.T * s.ld_u + c;
-    const T* pdt = static_cast<const T*>(s.dt) + b * s.T * s.ld_dt + c;
-    const T* pz = OUT && s.z ? static_cast<const T*>(s.z) + b * s.T * s.ld_z + c : nullptr;
+    // row 0 of this batch row and tile, the same in every lane
+    const T* pu = static_cast<const T*>(s.u) + b * s.T * s.ld_u + c0;
+    const T* pdt = static_cast<const T*>(s.dt) + b * s.T * s.ld_dt + c0;
+    const bool gated = OUT && s.z != nullptr;
+    const T* pz = gated ? static_cast<const T*>(s.z) + b * s.T * s.ld_z + c0 : nullptr;
     const T* pB = static_cast<const T*>(s.Bm) + b * s.T * s.ld_b + grp * N;
     const T* pC = static_cast<const T*>(s.Cm) + b * s.T * s.ld_c + grp * N;
+    T* py = y + b * s.T * s.D + c0;
+    const int64_t c = c0 + lc;
     const float bias = s.dt_bias ? s.dt_bias[c] : 0.f;
     const float h0 = OUT && s.h0 ? s.h0[c] : 0.f;
 
@@ -78,63 +97,83 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     }
     float total = 0.f;  // sum of the steps
 
-    float du[R], dd[R], dz[R], dr[PER];  // the next tile's values in flight
+    // The next tile's values, in flight as they lie in memory: a conversion would wait
+    // for them.  Rows past the last are its copies, so that no load is under a branch;
+    // their values are replaced by zeros when the tile is written to LDS.
+    T du[R], dd[R], dz[R], dr[PER];
+    int ej[PER], en[PER];  // the row and state of this thread's elements of B and C
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+        const int e = threadIdx.x + p * kWave * S, f = e % (S * W * NS);
+        ej[p] = e < E ? e / (S * W * NS) : 0;
+        en[p] = f / (W * NS) * NS + f % NS;
+        en[p] = (f / NS % W ? -1 : 1) * ((en[p] < N ? en[p] : N - 1) + 1);  // < 0: of C
+    }
     auto load = [&](int64_t t0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int64_t t = t0 + wave * R + r;
-            du[r] = dd[r] = dz[r] = 0.f;
-            if (t < te) {
-                du[r] = io_load(pu + t * s.ld_u);
-                dd[r] = io_load(pdt + t * s.ld_dt);
-                if (OUT && pz) dz[r] = io_load(pz + t * s.ld_z);
-            }
+            const int64_t t = t0 + wave * R + r < te ? t0 + wave * R + r : te - 1;
+            du[r] = (pu + t * s.ld_u)[lc];
+            dd[r] = (pdt + t * s.ld_dt)[lc];
+            if (gated) dz[r] = (pz + t * s.ld_z)[lc];
         }
+        const int64_t first = t0 < te ? t0 : te - 1;
+        const int last = int(te - 1 - first < kSteps ? te - 1 - first : kSteps);
+        const T *rB = pB + first * s.ld_b, *rC = pC + first * s.ld_c;
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            const int e = threadIdx.x + p * kWave * S;
-            const int j = e / (S * W * NS), f = e % (S * W * NS);
-            const int n = f / (W * NS) * NS + f % NS, which = f / NS % W;
-            dr[p] = 0.f;
-            if (e < E && t0 + j < te && n < N)
-                dr[p] = which ? io_load(pC + (t0 + j) * s.ld_c + n) : io_load(pB + (t0 + j) * s.ld_b + n);
+            const uint32_t j = ej[p] < last ? ej[p] : last;
+            if (!OUT || en[p] > 0)
+                dr[p] = rB[j * uint32_t(s.ld_b) + uint32_t(en[p] - 1)];
+            else
+                dr[p] = rC[j * uint32_t(s.ld_c) + uint32_t(-en[p] - 1)];
         }
     };
-    load(t_begin);
-    for (int64_t t0 = t_begin; t0 < te; t0 += kSteps) {
-        float cu[R], cz[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int j = wave * R + r;
-            // a step past the row's end is 0: the state stays
-            const float delta = t0 + j < te ? softplus(dd[r] + bias) : 0.f;
-            cu[r] = du[r];
-            cz[r] = dz[r];
-            step[j][lane] = make_float2(delta, delta * du[r]);
-        }
-#pragma unroll
-        for (int p = 0; p < PER; ++p) {
-            const int e = threadIdx.x + p * kWave * S;
-            if (e < E) (&rows[0][0][0][0])[e] = dr[p];
-        }
-        __syncthreads();
-        load(t0 + kSteps);
-#pragma unroll 4
+    // The steps of a tile for CNT states of this wavefront.  (Slots past N are not
+    // walked: zero times an infinite input is not zero.)
+    auto walk = [&](auto count) {
+        constexpr int CNT = decltype(count)::value;
+#pragma unroll 8
         for (int j = 0; j < kSteps; ++j) {
             const float2 d = step[j][lane];
             float acc = 0.f;
 #pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                const float a = exp2_fast(d.x * A2[i]);
-                x[i] = fmaf(a, x[i], d.y * rows[j][wave][0][i]);
-                // (slots past N take no part: 0 times an infinite input is not 0)
-                if constexpr (OUT) acc = i < real ? fmaf(rows[j][wave][W - 1][i], x[i], acc) : acc;
+            for (int i = 0; i < CNT; ++i) {
+                x[i] = fmaf(exp2_fast(d.x * A2[i]), x[i], d.y * rows[j][wave][0][i]);
+                if constexpr (OUT) acc = fmaf(rows[j][wave][W - 1][i], x[i], acc);
             }
             if constexpr (OUT)
                 part[wave][j][lane] = acc;
             else
                 total += d.x;
         }
+    };
+    if (t_begin < te) load(t_begin);
+    for (int64_t t0 = t_begin; t0 < te; t0 += kSteps) {
+        float cu[R], cz[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int j = wave * R + r;
+            cu[r] = io_load(&du[r]);
+            cz[r] = gated ? io_load(&dz[r]) : 0.f;
+            // a step past the row's end is 0: the state stays
+            float2 d;
+            d.x = softplus(io_load(&dd[r]) + bias);
+            d.y = d.x * cu[r];
+            step[j][lane] = t0 + j < te ? d : make_float2(0.f, 0.f);
+        }
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int e = threadIdx.x + p * kWave * S;
+            if (E % (kWave * S) == 0 || e < E)
+                (&rows[0][0][0][0])[e] = t0 + ej[p] < te ? io_load(&dr[p]) : 0.f;
+        }
+        __syncthreads();
+        load(t0 + kSteps);
+        if (real == NS)
+            walk(std::integral_constant<int, NS>());
+        else
+            with_count<NS - 1>(real, walk);
         __syncthreads();
         if constexpr (OUT) {
 #pragma unroll
@@ -143,14 +182,14 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
                 float o = h0 * cu[r];
 #pragma unroll
                 for (int w = 0; w < S; ++w) o += part[w][j][lane];
-                if (pz) o *= cz[r] * sigmoid(cz[r]);
-                if (own && t0 + j < te) io_store(y + (b * s.T + t0 + j) * s.D + c, o);
+                if (gated) o *= cz[r] * sigmoid(cz[r]);
+                if (own && t0 + j < te) io_store(py + (t0 + j) * s.D + lc, o);
             }
         }
     }
     if constexpr (OUT) {
         for (int64_t t = (te > t_begin ? te : t_begin) + wave; t < t_end; t += S)
-            if (own) io_store(y + (b * s.T + t) * s.D + c, 0.f);
+            if (own) io_store(py + t * s.D + lc, 0.f);
         if (k == nchunks - 1 && own) {
 #pragma unroll
             for (int i = 0; i < NS; ++i)

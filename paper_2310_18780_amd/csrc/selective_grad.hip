@@ -274,6 +274,13 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
         G[i] = i < p.real ? w.gs[at] : 0.f;
         dA[i] = 0.f;
     }
+    const float bias = s.dt_bias ? s.dt_bias[p.c] : 0.f, h0 = s.h0 ? s.h0[p.c] : 0.f;
+    float dh0 = 0.f, dbias = 0.f;
+    const int64_t row0 = p.b * s.T + p.t0;
+    // FULL: all NS slots hold states.  (Else the sums leave out the others, since zero
+    // times an infinite input is not zero.)
+    auto walk = [&](auto full) {
+    constexpr bool FULL = decltype(full)::value;
     // the state at the start of every block
     float start[kBlocks][NS];
 #pragma unroll
@@ -290,9 +297,6 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
             }
         }
     }
-    const float bias = s.dt_bias ? s.dt_bias[p.c] : 0.f, h0 = s.h0 ? s.h0[p.c] : 0.f;
-    float dh0 = 0.f, dbias = 0.f;
-    const int64_t row0 = p.b * s.T + p.t0;
 
 #pragma unroll 1
     for (int q = kBlocks - 1; q >= 0; --q) {
@@ -313,7 +317,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
                 a[j][i] = exp2_fast(delta * A2[i]);
                 before[j][i] = x[i];
                 x[i] = fmaf(a[j][i], x[i], du * m.B[j0 + j][p.n0 + i]);
-                if (i < p.real) o = fmaf(m.C[j0 + j][p.n0 + i], x[i], o);
+                if (FULL || i < p.real) o = fmaf(m.C[j0 + j][p.n0 + i], x[i], o);
             }
             if (gated) po[p.wave][j][p.lane] = o;
         }
@@ -331,7 +335,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
                 v[i] = G[i] * du;
                 v[NS + i] = d * after;
                 const float ag = a[j][i] * G[i], h = ag * before[j][i];
-                if (i < p.real) {
+                if (FULL || i < p.real) {
                     pv = fmaf(G[i], m.B[j0 + j][p.n0 + i], pv);
                     qv = fmaf(A[i], h, qv);
                 }
@@ -407,6 +411,11 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
         }
         __syncthreads();
     }
+    };
+    if (p.real == NS)
+        walk(std::true_type());
+    else
+        walk(std::false_type());
     // partial rows of the weights' gradients
     pp[p.wave][0][p.lane] = dh0;
     pp[p.wave][1][p.lane] = dbias;
