@@ -389,6 +389,7 @@ hipError_t norm_grad(const T* dy, const T* x, const float* w, const float* mean,
                      float* part, hipStream_t stream)
 {
     const int team = norm_team<T>(rows, D, true);
+    if (rows == 0) return launch_column_sum(part, 0, D, dw, D, db, 0, nullptr, stream);
     int64_t P;
     hipError_t e;
     if (team == 0) {
