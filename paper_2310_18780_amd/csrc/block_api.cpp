@@ -161,10 +161,11 @@ lh_status check_selective(const lh_selective_inputs* in, bool step, bool grad)
         (in->z && (s = check_ld("ld_z", in->ld_z, in->D, rows))) ||
         (s = check_ld("ld_B", in->ld_B, w, rows)) || (s = check_ld("ld_C", in->ld_C, w, rows)))
         return s;
-    // (a tile's rows of B and C are addressed in 32 bits)
-    for (const int64_t ld : {in->ld_B, in->ld_C})
-        if (ld >= (INT64_C(1) << 27))
-            return fail(LH_ERR_INVALID_ARG, "ld_B and ld_C must be < 2^27, got %lld", (long long)ld);
+    // (the rows of a tile are addressed in 32 bits)
+    for (const int64_t ld : {in->ld_dt, in->ld_u, in->z ? in->ld_z : 0, in->ld_B, in->ld_C})
+        if (ld >= (INT64_C(1) << 26))
+            return fail(LH_ERR_INVALID_ARG, "rows must be less than 2^26 elements apart, got %lld",
+                        (long long)ld);
     return LH_OK;
 }
 

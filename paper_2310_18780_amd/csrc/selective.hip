@@ -28,9 +28,18 @@ namespace {
 
 constexpr int kSteps = 16;  // steps of a tile
 
+// The element a 32-bit byte offset from a pointer that is the same in all lanes (which
+// the hardware adds by itself).
+template <typename T>
+__device__ __forceinline__ T& at_byte(T* p, uint32_t off)
+{
+    using C = std::conditional_t<std::is_const_v<T>, const char, char>;
+    return *reinterpret_cast<T*>(reinterpret_cast<C*>(p) + off);
+}
+
 // f with n as a constant, 0 <= n <= MOST (n < 0 is 0).
 template <int MOST, typename F>
-__device__ __forceinline__ void with_count(int n, F& f)
+__device__ __forceinline__ void with_count(int n, const F& f)
 {
     if constexpr (MOST <= 0) {
         f(std::integral_constant<int, 0>());
@@ -42,7 +51,7 @@ __device__ __forceinline__ void with_count(int n, F& f)
     }
 }
 
-template <typename T, int NS, int S, bool OUT>
+template <typename T, int NS, int S, bool OUT, bool GATE>
 __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chunk,
                                                         int64_t nchunks, float* xs, float* sums,
                                                         float* state, bool resume, T* y)
@@ -51,9 +60,9 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     constexpr int W = OUT ? 2 : 1;   // B (and C)
     constexpr int E = kSteps * S * W * NS;
     constexpr int PER = (E + kWave * S - 1) / (kWave * S);
-    __shared__ float2 step[kSteps][kWave];                    // delta, delta u
-    __shared__ __align__(16) float rows[kSteps][S][W][NS];    // B, C
-    __shared__ float part[OUT ? S : 1][kSteps][kWave];        // the wavefronts' parts of y
+    __shared__ float2 step[kSteps][kWave];                  // delta, delta u
+    __shared__ __align__(16) float rows[kSteps][S][W][NS];  // B, C
+    __shared__ float part[OUT ? S : 1][kSteps][kWave];      // the wavefronts' parts of y
 
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -63,7 +72,9 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     const int64_t k = rest % nchunks, b = rest / nchunks;
     const int64_t grp = tile / per, c0 = grp * Dg + (tile % per) * kWave;  // the tile's first channel
     const int width = int((grp + 1) * Dg - c0 < kWave ? (grp + 1) * Dg - c0 : kWave);
-    const bool own = lane < width;  // lanes past the group compute its last channel and store nothing
+    // Lanes past the group compute its last channel and store the same bits as its own
+    // lane, so that no store is under a mask.
+    const bool own = lane < width;
     const uint32_t lc = own ? lane : width - 1;
     const int n0 = wave * NS, real = N - n0 < NS ? N - n0 : NS;
 
@@ -74,8 +85,7 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     // row 0 of this batch row and tile, the same in every lane
     const T* pu = static_cast<const T*>(s.u) + b * s.T * s.ld_u + c0;
     const T* pdt = static_cast<const T*>(s.dt) + b * s.T * s.ld_dt + c0;
-    const bool gated = OUT && s.z != nullptr;
-    const T* pz = gated ? static_cast<const T*>(s.z) + b * s.T * s.ld_z + c0 : nullptr;
+    const T* pz = GATE ? static_cast<const T*>(s.z) + b * s.T * s.ld_z + c0 : nullptr;
     const T* pB = static_cast<const T*>(s.Bm) + b * s.T * s.ld_b + grp * N;
     const T* pC = static_cast<const T*>(s.Cm) + b * s.T * s.ld_c + grp * N;
     T* py = y + b * s.T * s.D + c0;
@@ -98,42 +108,59 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     float total = 0.f;  // sum of the steps
 
     // The next tile's values, in flight as they lie in memory: a conversion would wait
-    // for them.  Rows past the last are its copies, so that no load is under a branch;
-    // their values are replaced by zeros when the tile is written to LDS.
+    // for them.  A lane's places in a tile are 32-bit byte offsets from the tile's first row,
+    // the same for all tiles but the last, whose rows past the end are copies of the
+    // last (so that no load is under a branch) and become zeros in LDS.
     T du[R], dd[R], dz[R], dr[PER];
-    int ej[PER], en[PER];  // the row and state of this thread's elements of B and C
-#pragma unroll
-    for (int p = 0; p < PER; ++p) {
-        const int e = threadIdx.x + p * kWave * S, f = e % (S * W * NS);
-        ej[p] = e < E ? e / (S * W * NS) : 0;
-        en[p] = f / (W * NS) * NS + f % NS;
-        en[p] = (f / NS % W ? -1 : 1) * ((en[p] < N ? en[p] : N - 1) + 1);  // < 0: of C
-    }
-    auto load = [&](int64_t t0) {
+    uint32_t ou[R], od[R], oz[R], oe[PER];
+    int ej[PER];      // the row of this thread's elements of B and C
+    bool of_c[PER];
+    auto places = [&](int rows_left) {
+        const int last = rows_left < kSteps ? rows_left - 1 : kSteps - 1;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int64_t t = t0 + wave * R + r < te ? t0 + wave * R + r : te - 1;
-            du[r] = (pu + t * s.ld_u)[lc];
-            dd[r] = (pdt + t * s.ld_dt)[lc];
-            if (gated) dz[r] = (pz + t * s.ld_z)[lc];
+            const uint32_t j = wave * R + r < last ? wave * R + r : last;
+            ou[r] = (j * uint32_t(s.ld_u) + lc) * sizeof(T);
+            od[r] = (j * uint32_t(s.ld_dt) + lc) * sizeof(T);
+            oz[r] = (j * uint32_t(s.ld_z) + lc) * sizeof(T);
         }
-        const int64_t first = t0 < te ? t0 : te - 1;
-        const int last = int(te - 1 - first < kSteps ? te - 1 - first : kSteps);
-        const T *rB = pB + first * s.ld_b, *rC = pC + first * s.ld_c;
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
-            const uint32_t j = ej[p] < last ? ej[p] : last;
-            if (!OUT || en[p] > 0)
-                dr[p] = rB[j * uint32_t(s.ld_b) + uint32_t(en[p] - 1)];
-            else
-                dr[p] = rC[j * uint32_t(s.ld_c) + uint32_t(-en[p] - 1)];
+            const int e = threadIdx.x + p * kWave * S, f = e % (S * W * NS);
+            ej[p] = e < E ? e / (S * W * NS) : 0;
+            const int n = f / (W * NS) * NS + f % NS;
+            of_c[p] = f / NS % W;
+            oe[p] = (uint32_t(ej[p] < last ? ej[p] : last) * uint32_t(of_c[p] ? s.ld_c : s.ld_b) +
+                     (n < N ? n : N - 1)) * sizeof(T);
         }
+    };
+    // (the next tile's first row)
+    const T* nu = pu + t_begin * s.ld_u;
+    const T* nd = pdt + t_begin * s.ld_dt;
+    const T* nz = GATE ? pz + t_begin * s.ld_z : nullptr;
+    const T *nB = pB + t_begin * s.ld_b, *nC = pC + t_begin * s.ld_c;
+    auto load = [&]() {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            du[r] = at_byte(nu, ou[r]);
+            dd[r] = at_byte(nd, od[r]);
+            if constexpr (GATE) dz[r] = at_byte(nz, oz[r]);
+        }
+#pragma unroll
+        for (int p = 0; p < PER; ++p) dr[p] = at_byte(OUT && of_c[p] ? nC : nB, oe[p]);
+    };
+    auto advance = [&]() {
+        nu += kSteps * s.ld_u;
+        nd += kSteps * s.ld_dt;
+        if constexpr (GATE) nz += kSteps * s.ld_z;
+        nB += kSteps * s.ld_b;
+        nC += kSteps * s.ld_c;
     };
     // The steps of a tile for CNT states of this wavefront.  (Slots past N are not
     // walked: zero times an infinite input is not zero.)
     auto walk = [&](auto count) {
         constexpr int CNT = decltype(count)::value;
-#pragma unroll 8
+#pragma unroll
         for (int j = 0; j < kSteps; ++j) {
             const float2 d = step[j][lane];
             float acc = 0.f;
@@ -148,45 +175,63 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
                 total += d.x;
         }
     };
-    if (t_begin < te) load(t_begin);
-    for (int64_t t0 = t_begin; t0 < te; t0 += kSteps) {
+    // One tile: what is loaded goes to LDS, the next tile's loads start, this one is
+    // walked and its outputs leave.  TAIL: rows may be missing.
+    auto tile_steps = [&](int64_t t0, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        const int left = int(te - t0 < kSteps ? te - t0 : kSteps);
         float cu[R], cz[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int j = wave * R + r;
             cu[r] = io_load(&du[r]);
-            cz[r] = gated ? io_load(&dz[r]) : 0.f;
-            // a step past the row's end is 0: the state stays
+            if constexpr (GATE) cz[r] = io_load(&dz[r]);
             float2 d;
             d.x = softplus(io_load(&dd[r]) + bias);
             d.y = d.x * cu[r];
-            step[j][lane] = t0 + j < te ? d : make_float2(0.f, 0.f);
+            // a step past the row's end is 0: the state stays
+            if (TAIL && j >= left) d = make_float2(0.f, 0.f);
+            step[j][lane] = d;
         }
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             const int e = threadIdx.x + p * kWave * S;
             if (E % (kWave * S) == 0 || e < E)
-                (&rows[0][0][0][0])[e] = t0 + ej[p] < te ? io_load(&dr[p]) : 0.f;
+                (&rows[0][0][0][0])[e] = !TAIL || ej[p] < left ? io_load(&dr[p]) : 0.f;
         }
         __syncthreads();
-        load(t0 + kSteps);
+        const int64_t after = te - t0 - kSteps;  // rows left for the next tile
+        if (after > 0) {
+            advance();
+            if (after < kSteps) places(int(after));
+        }
+        load();  // (after the last tile: that tile again)
         if (real == NS)
             walk(std::integral_constant<int, NS>());
         else
             with_count<NS - 1>(real, walk);
         __syncthreads();
         if constexpr (OUT) {
+            T* row = py + t0 * s.D;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int j = wave * R + r;
                 float o = h0 * cu[r];
 #pragma unroll
                 for (int w = 0; w < S; ++w) o += part[w][j][lane];
-                if (gated) o *= cz[r] * sigmoid(cz[r]);
-                if (own && t0 + j < te) io_store(py + (t0 + j) * s.D + lc, o);
+                if constexpr (GATE) o *= cz[r] * sigmoid(cz[r]);
+                if (!TAIL || j < left)
+                    io_store(&at_byte(row, uint32_t(j) * uint32_t(s.D * sizeof(T)) + lc * uint32_t(sizeof(T))), o);
             }
         }
+    };
+    if (t_begin < te) {
+        places(int(te - t_begin < kSteps ? te - t_begin : kSteps));
+        load();
     }
+    int64_t t0 = t_begin;
+    for (; t0 + kSteps <= te; t0 += kSteps) tile_steps(t0, std::false_type());
+    if (t0 < te) tile_steps(t0, std::true_type());
     if constexpr (OUT) {
         for (int64_t t = (te > t_begin ? te : t_begin) + wave; t < t_end; t += S)
             if (own) io_store(py + t * s.D + lc, 0.f);
@@ -275,12 +320,11 @@ __global__ __launch_bounds__(256) void scan_step_kernel(Selective s, float* __re
     }
 }
 
-// States per lane and wavefronts per tile.
-void split_states(int N, int* ns, int* waves)
+// States per lane for this many wavefronts per tile.
+int states_per_lane(int N, int waves)
 {
-    *waves = N <= 16 ? 4 : N <= 32 ? 8 : 16;
-    *ns = (N + *waves - 1) / *waves;
-    if (*ns > 4) *ns = *ns <= 6 ? 6 : 8;
+    const int n = (N + waves - 1) / waves;
+    return n <= 4 ? n : n <= 6 ? 6 : 8;
 }
 
 template <typename F>
@@ -293,6 +337,8 @@ hipError_t with_split(int ns, int waves, F f)
     LH_SPLIT(2, 4);
     LH_SPLIT(3, 4);
     LH_SPLIT(4, 4);
+    LH_SPLIT(1, 8);
+    LH_SPLIT(2, 8);
     LH_SPLIT(3, 8);
     LH_SPLIT(4, 8);
     LH_SPLIT(3, 16);
@@ -314,7 +360,7 @@ hipError_t scan(const Selective& s, float* state, bool resume, T* y, void* works
     return with_split(p.ns, p.waves, [&](auto ns, auto waves) {
         constexpr int NS = decltype(ns)::value, S = decltype(waves)::value;
         if (p.nchunks > 1) {
-            hipLaunchKernelGGL((scan_kernel<T, NS, S, false>), dim3(uint32_t(blocks)),
+            hipLaunchKernelGGL((scan_kernel<T, NS, S, false, false>), dim3(uint32_t(blocks)),
                                dim3(kWave * S), 0, stream, s, p.chunk, p.nchunks, xs, sums, state,
                                resume, y);
             hipError_t e = hipGetLastError();
@@ -324,8 +370,9 @@ hipError_t scan(const Selective& s, float* state, bool resume, T* y, void* works
                                p.nchunks);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-        hipLaunchKernelGGL((scan_kernel<T, NS, S, true>), dim3(uint32_t(blocks)), dim3(kWave * S),
-                           0, stream, s, p.chunk, p.nchunks, xs, sums, state, resume, y);
+        const auto last = s.z ? scan_kernel<T, NS, S, true, true> : scan_kernel<T, NS, S, true, false>;
+        hipLaunchKernelGGL(last, dim3(uint32_t(blocks)), dim3(kWave * S), 0, stream, s, p.chunk,
+                           p.nchunks, xs, sums, state, resume, y);
         return hipGetLastError();
     });
 }
@@ -358,12 +405,25 @@ hipError_t scan_step(const Selective& s, float* state, T* y, hipStream_t stream)
 SelectivePlan selective_plan(int64_t B, int64_t T, int64_t D, int N, int G)
 {
     SelectivePlan p;
-    split_states(N, &p.ns, &p.waves);
-    const int64_t waves = B * group_tiles(D, G) * G * p.waves;
-    // two wavefronts per SIMD, chunks of 32 steps or more
-    int64_t n = waves >= 1024 ? 1 : (2048 + waves - 1) / waves;
+    const int64_t tiles = B * group_tiles(D, G) * G;
+    // One pass takes about 6 us and 0.1 us a step while the tiles leave the SIMDs waiting
+    // (8 wavefronts to a tile, up to 270 tiles; then in proportion); chunks take 14 us for
+    // three launches and, with the SIMDs full, 0.45 ns a step and tile at 16 states.
+    // (T = 2048, D = 2048, 16 states, one pass and chunks: 4 rows 199 and 133 us, 6 rows
+    // 200 and 194, 8 rows 199 and 232; 4 rows of 128 steps 18 and 25 us, 1 row of 256 steps
+    // 30 and 22 us.)
+    const double one = 6.0 + 0.1 * T * (tiles > 270 ? tiles / 270.0 : 1.0);
+    const double cut = 14.0 + 4.5e-4 * T * tiles * (N + 8) / 24;
+    // Chunks fill 8192 wavefronts (8 to a SIMD) where they stay 32 steps or longer.
+    const int wide = N <= 16 ? 4 : N <= 32 ? 8 : 16;
+    int64_t n = cut < one ? (8192 + tiles * wide - 1) / (tiles * wide) : 1;
     if (n > T / 32) n = T / 32;
     if (n < 3) n = 1;
+    // Up to 16 states, 4 wavefronts to a tile do the least work beside the states; in one
+    // pass of fewer than 1024 tiles 8 wait less (16 rows 299 against 345 us, 32 rows 560
+    // against 515).
+    p.waves = N <= 16 && n == 1 && tiles < 1024 ? 8 : wide;
+    p.ns = states_per_lane(N, p.waves);
     p.chunk = ((T + n - 1) / n + kSteps - 1) / kSteps * kSteps;
     if (p.chunk < kSteps) p.chunk = kSteps;
     p.nchunks = T > 0 ? (T + p.chunk - 1) / p.chunk : 1;

@@ -127,7 +127,7 @@ def test_selective_refusals():
     refused(INVALID, scan(Bm=None), "NULL")
     refused(INVALID, scan(state=None), "NULL")
     refused(INVALID, scan(ld_B=7), "ld_B")
-    refused(INVALID, scan(ld_C=1 << 27), "2^27")
+    refused(INVALID, scan(ld_C=1 << 26), "2^26")
     refused(INVALID, scan(ld_z=7), "ld_z")
     refused(DTYPE, scan(io_dtype=5))
     refused(OVERLAP, scan(y=A + 3 * MB), "y overlaps dt")
