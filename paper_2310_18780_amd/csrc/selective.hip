@@ -28,15 +28,6 @@ namespace {
 
 constexpr int kSteps = 16;  // steps of a tile
 
-// The element a 32-bit byte offset from a pointer that is the same in all lanes (which
-// the hardware adds by itself).
-template <typename T>
-__device__ __forceinline__ T& at_byte(T* p, uint32_t off)
-{
-    using C = std::conditional_t<std::is_const_v<T>, const char, char>;
-    return *reinterpret_cast<T*>(reinterpret_cast<C*>(p) + off);
-}
-
 // f with n as a constant, 0 <= n <= MOST (n < 0 is 0).
 template <int MOST, typename F>
 __device__ __forceinline__ void with_count(int n, const F& f)

@@ -52,6 +52,15 @@ size_t selective_grad_workspace_bytes(int64_t B, int64_t T, int64_t D, int N, in
 hipError_t launch_selective_grad(const Selective& s, const SelectiveGrads& g, void* workspace,
                                  hipStream_t stream);
 
+// The element a 32-bit byte offset from a pointer that is the same in all lanes (which
+// the hardware adds by itself).
+template <typename T>
+__device__ __forceinline__ T& at_byte(T* p, uint32_t off)
+{
+    using C = std::conditional_t<std::is_const_v<T>, const char, char>;
+    return *reinterpret_cast<T*>(reinterpret_cast<C*>(p) + off);
+}
+
 // Tokens of batch row b (a length outside [0, T] is taken as the nearer end).
 __device__ __forceinline__ int64_t tokens_of(const int* lengths, int64_t b, int64_t T)
 {

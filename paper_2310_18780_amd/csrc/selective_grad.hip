@@ -13,7 +13,7 @@
 // state from zero, the gradient that its own d hands to the state before it, and the
 // sum of steps; a carry turns both into what enters each chunk, from the past and from
 // the future.  The main pass walks a chunk forward once, keeping the state at the
-// start of each block of kBlockSteps steps, then takes the blocks from the last to
+// start of each block of 8 or 4 steps, then takes the blocks from the last to
 // the first: forward again with the states and decays of the block in registers, then
 // backward.  As in the prompt's scan a lane is a channel and the wavefronts of a
 // workgroup share out the states; p, q and o are summed over them in LDS.
@@ -27,9 +27,9 @@
 namespace lh {
 namespace {
 
-constexpr int kBlockSteps = 8;
-// Steps of a chunk: the block starts of a longer one take more registers (8 states to
-// a lane from 33 states on).
+// Steps of a block and of a chunk: what the registers hold of them, fewer with 8 states
+// to a lane (from 33 states on).
+constexpr int block_steps(int ns) { return ns < 8 ? 8 : 4; }
 constexpr int chunk_steps(int ns) { return ns < 8 ? 64 : 32; }
 
 struct GradWork {
@@ -42,8 +42,9 @@ struct GradWork {
 
 // What a lane needs to know of its place.
 struct Place {
-    int64_t tile, k, b, grp, c, t0, t1, te;
+    int64_t tile, k, b, grp, c0, c, t0, t1, te;
     int lane, wave, n0, real;
+    uint32_t lc;  // the lane's channel in the tile (past the group: the last)
     bool own;
 };
 
@@ -59,9 +60,11 @@ __device__ __forceinline__ Place place_of(const Selective& s, int64_t nchunks)
     p.k = rest % nchunks;
     p.b = rest / nchunks;
     p.grp = p.tile / per;
-    const int64_t cg = (p.tile % per) * kWave + p.lane;
-    p.own = cg < Dg;
-    p.c = p.grp * Dg + (p.own ? cg : Dg - 1);
+    p.c0 = p.grp * Dg + (p.tile % per) * kWave;
+    const int width = int((p.grp + 1) * Dg - p.c0 < kWave ? (p.grp + 1) * Dg - p.c0 : kWave);
+    p.own = p.lane < width;
+    p.lc = p.own ? p.lane : width - 1;
+    p.c = p.c0 + p.lc;
     p.n0 = p.wave * NS;
     p.real = s.N - p.n0 < NS ? s.N - p.n0 : NS;
     const int64_t len = tokens_of(s.lengths, p.b, s.T);
@@ -80,53 +83,77 @@ struct Chunk {
     float B[kChunk][S * NS], C[kChunk][S * NS];
 };
 
-template <typename T, int NS, int S>
+// Every load of a chunk starts before the first is used (rows past the last are its
+// copies, and become zeros in LDS: there the state stays).
+template <typename T, int NS, int S, bool GATE>
 __device__ __forceinline__ void load_chunk(const Selective& s, const SelectiveGrads& g,
                                            const Place& p, Chunk<S, NS>& m)
 {
-    constexpr int kChunk = chunk_steps(NS);
-    const T* pu = static_cast<const T*>(s.u) + p.b * s.T * s.ld_u + p.c;
-    const T* pdt = static_cast<const T*>(s.dt) + p.b * s.T * s.ld_dt + p.c;
-    const T* pz = s.z ? static_cast<const T*>(s.z) + p.b * s.T * s.ld_z + p.c : nullptr;
-    const T* pg = static_cast<const T*>(g.dy) + p.b * s.T * s.D + p.c;
-    const T* pB = static_cast<const T*>(s.Bm) + p.b * s.T * s.ld_b + p.grp * s.N;
-    const T* pC = static_cast<const T*>(s.Cm) + p.b * s.T * s.ld_c + p.grp * s.N;
+    constexpr int kChunk = chunk_steps(NS), R = kChunk / S;
+    constexpr int PER = (kChunk * NS + kWave - 1) / kWave;  // elements of B (of C) per thread
+    const int left = int(p.te - p.t0 < 0 ? 0 : p.te - p.t0);
+    const int64_t row0 = p.b * s.T + (left > 0 ? p.t0 : 0);
+    const int last = left > 0 ? left - 1 : 0;
+    const uint32_t off = p.lc * sizeof(T);
+    const T* pu = static_cast<const T*>(s.u) + row0 * s.ld_u + p.c0;
+    const T* pdt = static_cast<const T*>(s.dt) + row0 * s.ld_dt + p.c0;
+    const T* pz = GATE ? static_cast<const T*>(s.z) + row0 * s.ld_z + p.c0 : nullptr;
+    const T* pg = static_cast<const T*>(g.dy) + row0 * s.D + p.c0;
+    const T* pB = static_cast<const T*>(s.Bm) + row0 * s.ld_b + p.grp * s.N;
+    const T* pC = static_cast<const T*>(s.Cm) + row0 * s.ld_c + p.grp * s.N;
     const float bias = s.dt_bias ? s.dt_bias[p.c] : 0.f;
-#pragma unroll 4
-    for (int j = p.wave; j < kChunk; j += S) {
-        const int64_t t = p.t0 + j;
-        float delta = 0.f, du = 0.f, d = 0.f;  // past the row's end the state stays
-        if (t < p.te) {
-            delta = softplus(io_load(pdt + t * s.ld_dt) + bias);
-            du = delta * io_load(pu + t * s.ld_u);
-            d = io_load(pg + t * s.D);
-            if (pz) {
-                const float z = io_load(pz + t * s.ld_z);
-                d *= z * sigmoid(z);
-            }
-            // (lanes past the group add nothing to the sums over channels)
-            if (!p.own) d = 0.f, du = 0.f;
+    T ru[R], rd[R], rz[R], rg[R], rB[PER], rC[PER];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int64_t j = p.wave + i * S < last ? p.wave + i * S : last;
+        ru[i] = at_byte(pu + j * s.ld_u, off);
+        rd[i] = at_byte(pdt + j * s.ld_dt, off);
+        rg[i] = at_byte(pg + j * s.D, off);
+        if constexpr (GATE) rz[i] = at_byte(pz + j * s.ld_z, off);
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = threadIdx.x + i * kWave * S;
+        const int64_t j = e / (S * NS) < last ? e / (S * NS) : last;
+        const int n = e % (S * NS) < s.N ? e % (S * NS) : s.N - 1;
+        rB[i] = pB[j * s.ld_b + n];
+        rC[i] = pC[j * s.ld_c + n];
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int j = p.wave + i * S;
+        float delta = softplus(io_load(&rd[i]) + bias);
+        float du = delta * io_load(&ru[i]), d = io_load(&rg[i]);
+        if constexpr (GATE) {
+            const float z = io_load(&rz[i]);
+            d *= z * sigmoid(z);
         }
+        if (j >= left) delta = du = d = 0.f;
+        // (lanes past the group add nothing to the sums over channels)
+        if (!p.own) du = d = 0.f;
         m.delta[j][p.lane] = delta;
         m.du[j][p.lane] = du;
         m.d[j][p.lane] = d;
     }
-    for (int e = threadIdx.x; e < kChunk * S * NS; e += kWave * S) {
-        const int j = e / (S * NS), n = e % (S * NS);
-        const bool in = p.t0 + j < p.te && n < s.N;
-        m.B[j][n] = in ? io_load(pB + (p.t0 + j) * s.ld_b + n) : 0.f;
-        m.C[j][n] = in ? io_load(pC + (p.t0 + j) * s.ld_c + n) : 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = threadIdx.x + i * kWave * S, j = e / (S * NS), n = e % (S * NS);
+        if (e < kChunk * S * NS) {
+            const bool in = j < left && n < s.N;
+            m.B[j][n] = in ? io_load(&rB[i]) : 0.f;
+            m.C[j][n] = in ? io_load(&rC[i]) : 0.f;
+        }
     }
     __syncthreads();
 }
 
-template <typename T, int NS, int S>
+template <typename T, int NS, int S, bool GATE>
 __global__ __launch_bounds__(kWave* S) void grad_ends_kernel(Selective s, SelectiveGrads g,
                                                              GradWork w, int64_t nchunks)
 {
     __shared__ Chunk<S, NS> m;
     const Place p = place_of<NS>(s, nchunks);
-    load_chunk<T, NS, S>(s, g, p, m);
+    load_chunk<T, NS, S, GATE>(s, g, p, m);
     float A2[NS], x[NS], dec[NS], r[NS], total = 0.f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
@@ -253,16 +280,16 @@ __device__ __forceinline__ float sum_below(float v, int lane)
     }
 }
 
-template <typename T, int NS, int S>
+template <typename T, int NS, int S, bool GATE>
 __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGrads g, GradWork w,
                                                         int64_t nchunks)
 {
+    constexpr int kBlockSteps = block_steps(NS);
     __shared__ Chunk<S, NS> m;
-    __shared__ float po[S][kBlockSteps][kWave], pp[S][kBlockSteps][kWave], pq[S][kBlockSteps][kWave];
+    __shared__ float po[GATE ? S : 1][kBlockSteps][kWave], pp[S][kBlockSteps][kWave], pq[S][kBlockSteps][kWave];
     const Place p = place_of<NS>(s, nchunks);
     constexpr int kBlocks = chunk_steps(NS) / kBlockSteps;
-    const bool gated = s.z != nullptr;
-    load_chunk<T, NS, S>(s, g, p, m);
+    load_chunk<T, NS, S, GATE>(s, g, p, m);
 
     float A[NS], A2[NS], x[NS], G[NS], dA[NS];
 #pragma unroll
@@ -276,7 +303,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
     }
     const float bias = s.dt_bias ? s.dt_bias[p.c] : 0.f, h0 = s.h0 ? s.h0[p.c] : 0.f;
     float dh0 = 0.f, dbias = 0.f;
-    const int64_t row0 = p.b * s.T + p.t0;
+    const int64_t row0 = p.b * s.T + p.t0, last = p.t1 - 1 - p.t0;
     // FULL: all NS slots hold states.  (Else the sums leave out the others, since zero
     // times an infinite input is not zero.)
     auto walk = [&](auto full) {
@@ -308,6 +335,20 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
                 for (int i = 0; i < NS; ++i) x[i] = start[z][i];
         float before[kBlockSteps][NS], a[kBlockSteps][NS];
         const int j0 = q * kBlockSteps;
+        // what this wavefront's rows of the block need beside the sums, loaded ahead
+        constexpr int kRows = (kBlockSteps + S - 1) / S;
+        T ru[kRows], rd[kRows], rz[kRows], rg[kRows];
+        const uint32_t off = p.lc * sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int64_t j = j0 + p.wave + i * S < last ? j0 + p.wave + i * S : last;
+            ru[i] = at_byte(static_cast<const T*>(s.u) + (row0 + j) * s.ld_u + p.c0, off);
+            rd[i] = at_byte(static_cast<const T*>(s.dt) + (row0 + j) * s.ld_dt + p.c0, off);
+            if constexpr (GATE) {
+                rz[i] = at_byte(static_cast<const T*>(s.z) + (row0 + j) * s.ld_z + p.c0, off);
+                rg[i] = at_byte(static_cast<const T*>(g.dy) + (row0 + j) * s.D + p.c0, off);
+            }
+        }
 #pragma unroll
         for (int j = 0; j < kBlockSteps; ++j) {
             const float delta = m.delta[j0 + j][p.lane], du = m.du[j0 + j][p.lane];
@@ -319,7 +360,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
                 x[i] = fmaf(a[j][i], x[i], du * m.B[j0 + j][p.n0 + i]);
                 if (FULL || i < p.real) o = fmaf(m.C[j0 + j][p.n0 + i], x[i], o);
             }
-            if (gated) po[p.wave][j][p.lane] = o;
+            if constexpr (GATE) po[p.wave][j][p.lane] = o;
         }
         float folded[kBlockSteps];
         constexpr int kTop = 64 / (2 * NS);  // lane bits below kTop are left after a step's folds
@@ -374,14 +415,19 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
         }
         __syncthreads();
         // the channels' gradients of the block's steps, shared out among the wavefronts
-        for (int j = p.wave; j < kBlockSteps; j += S) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int j = p.wave + i * S;
             const int64_t t = p.t0 + j0 + j;
-            if (t >= p.t1 || !p.own) continue;
-            const int64_t at = (row0 + j0 + j) * s.D + p.c;
+            if (j >= kBlockSteps || t >= p.t1 || !p.own) continue;
+            const int64_t row = (row0 + j0 + j) * s.D + p.c0;
+            T& ddt_at = at_byte(static_cast<T*>(g.ddt) + row, off);
+            T& du_at = at_byte(static_cast<T*>(g.du) + row, off);
+            T& dz_at = GATE ? at_byte(static_cast<T*>(g.dz) + row, off) : du_at;
             if (t >= p.te) {
-                io_store(static_cast<T*>(g.du) + at, 0.f);
-                io_store(static_cast<T*>(g.ddt) + at, 0.f);
-                if (gated) io_store(static_cast<T*>(g.dz) + at, 0.f);
+                io_store(&du_at, 0.f);
+                io_store(&ddt_at, 0.f);
+                if constexpr (GATE) io_store(&dz_at, 0.f);
                 continue;
             }
             float pv = 0.f, qv = 0.f;
@@ -390,23 +436,18 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
                 pv += pp[k][j][p.lane];
                 qv += pq[k][j][p.lane];
             }
-            const int64_t row = row0 + j0 + j;
-            const float u = io_load(static_cast<const T*>(s.u) + row * s.ld_u + p.c);
-            const float d = m.d[j0 + j][p.lane];
-            const float slope = sigmoid(io_load(static_cast<const T*>(s.dt) + row * s.ld_dt + p.c) + bias);
-            const float ddt = fmaf(u, pv, qv) * slope;
-            io_store(static_cast<T*>(g.ddt) + at, ddt);
-            io_store(static_cast<T*>(g.du) + at, fmaf(m.delta[j0 + j][p.lane], pv, h0 * d));
+            const float u = io_load(&ru[i]), d = m.d[j0 + j][p.lane];
+            const float ddt = fmaf(u, pv, qv) * sigmoid(io_load(&rd[i]) + bias);
+            io_store(&ddt_at, ddt);
+            io_store(&du_at, fmaf(m.delta[j0 + j][p.lane], pv, h0 * d));
             dbias += ddt;
             dh0 = fmaf(d, u, dh0);
-            if (gated) {
+            if constexpr (GATE) {
                 float o = h0 * u;
 #pragma unroll
                 for (int k = 0; k < S; ++k) o += po[k][j][p.lane];
-                const float z = io_load(static_cast<const T*>(s.z) + row * s.ld_z + p.c);
-                const float sg = sigmoid(z);
-                io_store(static_cast<T*>(g.dz) + at,
-                         io_load(static_cast<const T*>(g.dy) + at) * o * (sg * fmaf(z, 1.f - sg, 1.f)));
+                const float z = io_load(&rz[i]), sg = sigmoid(z);
+                io_store(&dz_at, io_load(&rg[i]) * o * (sg * fmaf(z, 1.f - sg, 1.f)));
             }
         }
         __syncthreads();
@@ -523,15 +564,15 @@ hipError_t scan_grad(const Selective& s, const SelectiveGrads& g, void* workspac
         const dim3 grid(uint32_t(s.B * n * tiles));
         e = with_grad_split(ns, waves, [&](auto a, auto b) {
             constexpr int NS = decltype(a)::value, S = decltype(b)::value;
-            hipLaunchKernelGGL((grad_ends_kernel<T, NS, S>), grid, dim3(kWave * S), 0, stream, s, g,
-                               w, n);
+            const auto ends = s.z ? grad_ends_kernel<T, NS, S, true> : grad_ends_kernel<T, NS, S, false>;
+            const auto main = s.z ? grad_kernel<T, NS, S, true> : grad_kernel<T, NS, S, false>;
+            hipLaunchKernelGGL(ends, grid, dim3(kWave * S), 0, stream, s, g, w, n);
             hipError_t r = hipGetLastError();
             if (r != hipSuccess) return r;
             hipLaunchKernelGGL(grad_carry_kernel, dim3(uint32_t((2 * s.B * s.D * s.N + 255) / 256)),
                                dim3(256), 0, stream, s.A, w, s.B, s.D, s.N, n);
             if ((r = hipGetLastError()) != hipSuccess) return r;
-            hipLaunchKernelGGL((grad_kernel<T, NS, S>), grid, dim3(kWave * S), 0, stream, s, g, w,
-                               n);
+            hipLaunchKernelGGL(main, grid, dim3(kWave * S), 0, stream, s, g, w, n);
             return hipGetLastError();
         });
         if (e != hipSuccess) return e;
