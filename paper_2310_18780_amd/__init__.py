@@ -508,6 +508,10 @@ def _ptr(t):
 def _need_rows(t, name, dtype, lead, row) -> int:
     """Checks ``t`` of shape ``lead + row`` (``lead``: ``(B, T)`` or ``(B,)``): contiguous
     rows, a fixed distance apart; returns that distance in elements."""
+    # one test of all properties of a contiguous tensor, as in _need
+    if (isinstance(t, _torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == lead + row
+            and t.is_contiguous()):
+        return row[0] if len(row) == 1 else row[0] * row[1]
     if not isinstance(t, _torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:

@@ -27,63 +27,51 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return __builtin_bit_cast(uint32_t, v);
 }
 
-// V consecutive elements, V * sizeof(T) = 16 or 8 bytes.
-template <int V>
-__device__ __forceinline__ void load_piece(const float* p, float (&v)[V])
+// A piece of V values as it lies in memory (16 or 8 bytes, or one value), and its
+// values.  (A piece that is converted where it is loaded is waited for there.)
+template <typename T, int V>
+struct RawOf {
+    using type = std::conditional_t<V * sizeof(T) == 16, piece4, piece2>;
+};
+template <typename T>
+struct RawOf<T, 1> {
+    using type = T;
+};
+template <typename T, int V>
+using Raw = typename RawOf<T, V>::type;
+
+template <int V, typename T>
+__device__ __forceinline__ Raw<T, V> load_raw(const T* p)
 {
-    static_assert(V == 4 || V == 2, "16 or 8 bytes");
-    if constexpr (V == 4) {
-        const piece4 r = *reinterpret_cast<const piece4*>(p);
-        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
-    } else {
-        const piece2 r = *reinterpret_cast<const piece2*>(p);
-        for (int i = 0; i < 2; ++i) v[i] = __uint_as_float(r[i]);
-    }
+    return *reinterpret_cast<const Raw<T, V>*>(p);
 }
-template <int V>
-__device__ __forceinline__ void load_piece(const bf16* p, float (&v)[V])
+template <int V, typename T>
+__device__ __forceinline__ void expand(const Raw<T, V>& r, float (&v)[V])
 {
-    static_assert(V == 8 || V == 4, "16 or 8 bytes");
-    if constexpr (V == 8) {
-        const piece4 r = *reinterpret_cast<const piece4*>(p);
-        for (int i = 0; i < 4; ++i) {
+    if constexpr (V == 1) {
+        v[0] = io_load(&r);
+    } else if constexpr (sizeof(T) == 4) {
+        for (int i = 0; i < V; ++i) v[i] = __uint_as_float(r[i]);
+    } else {
+        for (int i = 0; i < V / 2; ++i) {
             v[2 * i] = __uint_as_float(r[i] << 16);
             v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
         }
-    } else {
-        const piece2 r = *reinterpret_cast<const piece2*>(p);
-        for (int i = 0; i < 2; ++i) {
-            v[2 * i] = __uint_as_float(r[i] << 16);
-            v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
-        }
     }
 }
-template <int V>
-__device__ __forceinline__ void store_piece(float* p, const float (&v)[V])
+template <int V, typename T>
+__device__ __forceinline__ void put(T* p, const float (&v)[V])
 {
-    static_assert(V == 4 || V == 2, "16 or 8 bytes");
-    if constexpr (V == 4) {
-        piece4 r;
-        for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(v[i]);
-        *reinterpret_cast<piece4*>(p) = r;
+    if constexpr (V == 1) {
+        io_store(p, v[0]);
+    } else if constexpr (sizeof(T) == 4) {
+        Raw<T, V> r;
+        for (int i = 0; i < V; ++i) r[i] = __float_as_uint(v[i]);
+        *reinterpret_cast<Raw<T, V>*>(p) = r;
     } else {
-        piece2 r;
-        for (int i = 0; i < 2; ++i) r[i] = __float_as_uint(v[i]);
-        *reinterpret_cast<piece2*>(p) = r;
-    }
-}
-template <int V>
-__device__ __forceinline__ void store_piece(bf16* p, const float (&v)[V])
-{
-    static_assert(V == 8 || V == 4, "16 or 8 bytes");
-    if constexpr (V == 8) {
-        piece4 r;
-        for (int i = 0; i < 4; ++i) r[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<piece4*>(p) = r;
-    } else {
-        piece2 r;
-        for (int i = 0; i < 2; ++i) r[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<piece2*>(p) = r;
+        Raw<T, V> r;
+        for (int i = 0; i < V / 2; ++i) r[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<Raw<T, V>*>(p) = r;
     }
 }
 
@@ -92,7 +80,7 @@ template <int V, typename T>
 __device__ __forceinline__ void load_some(const T* p, int n, float (&v)[V])
 {
     if (n >= V) {
-        load_piece<V>(p, v);
+        expand<V, T>(load_raw<V>(p), v);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = i < n ? io_load(p + i) : 0.f;
@@ -102,7 +90,7 @@ template <int V, typename T>
 __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[V])
 {
     if (n >= V) {
-        store_piece<V>(p, v);
+        put<V>(p, v);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)

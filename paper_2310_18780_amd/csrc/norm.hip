@@ -24,10 +24,10 @@ namespace {
 // holds five arrays of them).
 constexpr int hold(int team, bool grad)
 {
-    return grad ? (team == 64 ? 32 : team == 256 ? 16 : 8) : (team == 1024 ? 16 : 32);
+    return grad ? (team == 1024 ? 8 : 16) : (team == 1024 ? 16 : 32);
 }
 constexpr int64_t kMaxBlocks = 1 << 20;  // grid-stride beyond
-constexpr int64_t kGradBlocks = 512;  // workgroups (partial rows) of the gradient
+constexpr int64_t kGradBlocks = 1024;  // workgroups (partial rows) of the gradient
 
 constexpr int norm_block(int team) { return team < 256 ? 256 : team; }
 
@@ -52,7 +52,26 @@ __device__ __forceinline__ float2 team_sum(float2 v, float2* red)
     return v;
 }
 
-template <typename T, int TEAM, int ITER>
+// A lane's pieces of a row: ITER pieces of V values, TEAM pieces apart.  A piece that
+// would pass the row's end starts V values before it instead, so that every load is a
+// whole piece under no branch; its first `twice` values are another lane's as well, and
+// take no part in sums.  (Both lanes store the same bits.)  FULL: no such piece.
+template <int V, int TEAM, int ITER, bool FULL>
+struct Pieces {
+    int at[ITER], twice[ITER];
+    __device__ __forceinline__ Pieces(int lane, int D)
+    {
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            const int c = (i * TEAM + lane) * V;
+            at[i] = FULL || c + V <= D ? c : D - V;
+            twice[i] = c - at[i];
+        }
+    }
+    __device__ __forceinline__ bool mine(int i, int j) const { return FULL || j >= twice[i]; }
+};
+
+template <typename T, int TEAM, int ITER, bool FULL>
 __global__ __launch_bounds__(norm_block(TEAM)) void norm_kernel(
     const T* x, const T* residual, const float* __restrict__ w, const float* __restrict__ b,
     T* __restrict__ y, T* total, float* __restrict__ mean, float* __restrict__ rstd, int64_t rows,
@@ -60,68 +79,57 @@ __global__ __launch_bounds__(norm_block(TEAM)) void norm_kernel(
 {
     constexpr int V = kVec<T>;
     constexpr int teams = norm_block(TEAM) / TEAM;
-    __shared__ float2 red[3][norm_block(TEAM) / kWave];
+    __shared__ float2 red[2][norm_block(TEAM) / kWave];
     const int lane = threadIdx.x % TEAM;
+    const Pieces<V, TEAM, ITER, FULL> p(lane, D);
     const int64_t step = int64_t(gridDim.x) * teams;
     for (int64_t row = int64_t(blockIdx.x) * teams + threadIdx.x / TEAM; row < rows; row += step) {
-        const T* px = x + row * D;
-        float v[ITER][V];
+        Raw<T, V> raw[ITER], res[ITER];
 #pragma unroll
-        for (int i = 0; i < ITER; ++i)
-            load_some<V>(px + (i * TEAM + lane) * V, D - (i * TEAM + lane) * V, v[i]);
+        for (int i = 0; i < ITER; ++i) raw[i] = load_raw<V>(x + row * D + p.at[i]);
         if (residual) {
 #pragma unroll
-            for (int i = 0; i < ITER; ++i) {
+            for (int i = 0; i < ITER; ++i) res[i] = load_raw<V>(residual + row * D + p.at[i]);
+        }
+        float v[ITER][V], s = 0.f;
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+            expand<V, T>(raw[i], v[i]);
+            if (residual) {
                 float r[V];
-                load_some<V>(residual + row * D + (i * TEAM + lane) * V, D - (i * TEAM + lane) * V,
-                             r);
+                expand<V, T>(res[i], r);
 #pragma unroll
                 for (int j = 0; j < V; ++j) v[i][j] += r[j];
             }
-        }
-        if (total) {
 #pragma unroll
-            for (int i = 0; i < ITER; ++i)
-                store_some<V>(total + row * D + (i * TEAM + lane) * V, D - (i * TEAM + lane) * V,
-                              v[i]);
+            for (int j = 0; j < V; ++j) s += p.mine(i, j) ? v[i][j] : 0.f;
         }
-        float s = 0.f;
+        const float m = team_sum<TEAM>(make_float2(s, 0.f), red[0]).x / D;
+        if (total) {  // (in place of x or residual: the whole team has read them by now)
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) put<V>(total + row * D + p.at[i], v[i]);
+        }
+        float q = 0.f;
 #pragma unroll
         for (int i = 0; i < ITER; ++i)
 #pragma unroll
-            for (int j = 0; j < V; ++j) s += v[i][j];
-        const float m = team_sum<TEAM>(make_float2(s, 0.f), red[0]).x / D;
-        float q = 0.f;
-#pragma unroll
-        for (int i = 0; i < ITER; ++i) {
-            const int n = D - (i * TEAM + lane) * V;
-#pragma unroll
             for (int j = 0; j < V; ++j) {
                 v[i][j] -= m;
-                if (j < n) q = fmaf(v[i][j], v[i][j], q);
+                q = fmaf(p.mine(i, j) ? v[i][j] : 0.f, v[i][j], q);
             }
-        }
         const float var = team_sum<TEAM>(make_float2(q, 0.f), red[1]).x / D;
         const float rs = 1.f / sqrtf(var + eps);
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = (i * TEAM + lane) * V;
-            float wv[V], bv[V];
-            if (c + V <= D) {
+            const float *pw = w + p.at[i], *pb = b ? b + p.at[i] : nullptr;
+            float o[V];
 #pragma unroll
-                for (int j = 0; j < V; ++j) wv[j] = w[c + j];
+            for (int j = 0; j < V; ++j) o[j] = v[i][j] * rs * pw[j];
+            if (b) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) bv[j] = b ? b[c + j] : 0.f;
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    wv[j] = c + j < D ? w[c + j] : 0.f;
-                    bv[j] = b && c + j < D ? b[c + j] : 0.f;
-                }
+                for (int j = 0; j < V; ++j) o[j] += pb[j];
             }
-#pragma unroll
-            for (int j = 0; j < V; ++j) wv[j] = fmaf(v[i][j] * rs, wv[j], bv[j]);
-            store_some<V>(y + row * D + c, D - c, wv);
+            put<V>(y + row * D + p.at[i], o);
         }
         if (lane == 0) {
             if (mean) mean[row] = m;
@@ -183,7 +191,7 @@ __global__ __launch_bounds__(1024) void norm_wide_kernel(
     }
 }
 
-template <typename T, int TEAM, int ITER>
+template <typename T, int TEAM, int ITER, bool FULL>
 __global__ __launch_bounds__(norm_block(TEAM)) void norm_grad_kernel(
     const T* __restrict__ dy, const T* __restrict__ x, const float* __restrict__ w,
     const float* __restrict__ mean, const float* __restrict__ rstd, const T* dtotal, T* dx,
@@ -193,39 +201,45 @@ __global__ __launch_bounds__(norm_block(TEAM)) void norm_grad_kernel(
     constexpr int teams = norm_block(TEAM) / TEAM;
     __shared__ float2 red[2][norm_block(TEAM) / kWave];
     const int lane = threadIdx.x % TEAM;
+    const Pieces<V, TEAM, ITER, FULL> p(lane, D);
     const float inv = 1.f / D;
     float wv[ITER][V], aw[ITER][V], ab[ITER][V];
 #pragma unroll
     for (int i = 0; i < ITER; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int c = (i * TEAM + lane) * V + j;
-            wv[i][j] = c < D ? w[c] : 0.f;
+            wv[i][j] = w[p.at[i] + j];
             aw[i][j] = ab[i][j] = 0.f;
         }
     const int64_t step = int64_t(gridDim.x) * teams;
     int turn = 0;
     for (int64_t row = int64_t(blockIdx.x) * teams + threadIdx.x / TEAM; row < rows; row += step) {
-        const float m = mean[row], rs = rstd[row];
-        float h[ITER][V], g[ITER][V];
+        Raw<T, V> rx[ITER], rg[ITER], rt[ITER];
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = (i * TEAM + lane) * V;
-            load_some<V>(x + row * D + c, D - c, h[i]);
-            load_some<V>(dy + row * D + c, D - c, g[i]);
+            rx[i] = load_raw<V>(x + row * D + p.at[i]);
+            rg[i] = load_raw<V>(dy + row * D + p.at[i]);
         }
+        if (dtotal) {  // (read before the team's sum: dx may be its buffer)
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) rt[i] = load_raw<V>(dtotal + row * D + p.at[i]);
+        }
+        const float m = mean[row], rs = rstd[row];
+        float h[ITER][V], g[ITER][V];
         float2 s = make_float2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int n = D - (i * TEAM + lane) * V;
+            expand<V, T>(rx[i], h[i]);
+            expand<V, T>(rg[i], g[i]);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                h[i][j] = j < n ? (h[i][j] - m) * rs : 0.f;
+                h[i][j] = (h[i][j] - m) * rs;
                 aw[i][j] = fmaf(g[i][j], h[i][j], aw[i][j]);
                 ab[i][j] += g[i][j];
                 g[i][j] *= wv[i][j];
-                s.x += g[i][j];
-                s.y = fmaf(g[i][j], h[i][j], s.y);
+                const float own = p.mine(i, j) ? g[i][j] : 0.f;
+                s.x += own;
+                s.y = fmaf(own, h[i][j], s.y);
             }
         }
         s = team_sum<TEAM>(s, red[turn]);
@@ -233,15 +247,14 @@ __global__ __launch_bounds__(norm_block(TEAM)) void norm_grad_kernel(
         const float mg = s.x * inv, mgh = s.y * inv;
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = (i * TEAM + lane) * V;
             float t[V];
-            if (dtotal) load_some<V>(dtotal + row * D + c, D - c, t);
+            if (dtotal) expand<V, T>(rt[i], t);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float d = rs * (g[i][j] - fmaf(h[i][j], mgh, mg));
                 h[i][j] = dtotal ? d + t[j] : d;
             }
-            store_some<V>(dx + row * D + c, D - c, h[i]);
+            put<V>(dx + row * D + p.at[i], h[i]);
         }
     }
     // one partial row [2, D] per workgroup
@@ -249,31 +262,31 @@ __global__ __launch_bounds__(norm_block(TEAM)) void norm_grad_kernel(
     if constexpr (teams == 1) {
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
-            const int c = (i * TEAM + lane) * V;
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (c + j < D) {
-                    out[c + j] = aw[i][j];
-                    out[D + c + j] = ab[i][j];
+                if (p.mine(i, j)) {
+                    out[p.at[i] + j] = aw[i][j];
+                    out[D + p.at[i] + j] = ab[i][j];
                 }
         }
     } else {
-        __shared__ float sum[teams][2][kWave * V];
+        // the teams' sums of a lane's columns, added (TEAM is a wavefront)
+        __shared__ float sum[teams][2][V][kWave];
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                sum[threadIdx.x / TEAM][0][lane * V + j] = aw[i][j];
-                sum[threadIdx.x / TEAM][1][lane * V + j] = ab[i][j];
+                sum[threadIdx.x / TEAM][0][j][lane] = aw[i][j];
+                sum[threadIdx.x / TEAM][1][j][lane] = ab[i][j];
             }
             __syncthreads();
-            for (int k = threadIdx.x; k < 2 * kWave * V; k += norm_block(TEAM)) {
-                const int which = k / (kWave * V), c = i * TEAM * V + k % (kWave * V);
+            for (int k = threadIdx.x / TEAM; k < 2 * V; k += teams) {
+                const int which = k / V, j = k % V;
                 float a = 0.f;
 #pragma unroll
-                for (int t = 0; t < teams; ++t) a += sum[t][which][k % (kWave * V)];
-                if (c < D) out[int64_t(which) * D + c] = a;
+                for (int t = 0; t < teams; ++t) a += sum[t][which][j][lane];
+                if (p.mine(i, j)) out[int64_t(which) * D + p.at[i] + j] = a;
             }
         }
     }
@@ -325,11 +338,11 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(
     part[int64_t(blockIdx.y) * 2 * D + D + c] = ab;
 }
 
-// Wavefronts per row: one where there are rows enough to fill the GPU (two per
-// SIMD), else the fewest lanes' work per row, so that a few rows finish soon.
+// Threads per row (0: the wide kernels).
 template <typename T>
 int norm_team(int64_t rows, int64_t D, bool grad)
 {
+    if (D < kVec<T>) return 0;
     if (D <= 64 * hold(64, grad) && (rows >= 2048 || D <= 64 * kVec<T>)) return 64;
     if (D <= 256 * hold(256, grad) && (rows >= 512 || D <= 256 * kVec<T>)) return 256;
     return D <= 1024 * hold(1024, grad) ? 1024 : 0;
@@ -342,13 +355,17 @@ hipError_t with_shape(int team, int64_t D, F f)
     const int64_t pieces = (D + int64_t(team) * kVec<T> - 1) / (int64_t(team) * kVec<T>);
     auto iters = [&](auto t) {
         constexpr int most = hold(decltype(t)::value, GRAD) / kVec<T>;
+        auto full = [&](auto it) {
+            if (D == int64_t(team) * kVec<T> * decltype(it)::value) return f(t, it, std::true_type());
+            return f(t, it, std::false_type());
+        };
         if constexpr (most > 1)
-            if (pieces <= 1) return f(t, std::integral_constant<int, 1>());
+            if (pieces <= 1) return full(std::integral_constant<int, 1>());
         if constexpr (most > 2)
-            if (pieces <= 2) return f(t, std::integral_constant<int, 2>());
+            if (pieces <= 2) return full(std::integral_constant<int, 2>());
         if constexpr (most > 4)
-            if (pieces <= 4) return f(t, std::integral_constant<int, 4>());
-        return f(t, std::integral_constant<int, most>());
+            if (pieces <= 4) return full(std::integral_constant<int, 4>());
+        return full(std::integral_constant<int, most>());
     };
     if (team == 64) return iters(std::integral_constant<int, 64>());
     if (team == 256) return iters(std::integral_constant<int, 256>());
@@ -373,9 +390,10 @@ hipError_t norm(const T* x, const T* residual, const float* w, const float* b, T
                            eps);
         return hipGetLastError();
     }
-    return with_shape<T, false>(team, D, [&](auto t, auto it) {
+    return with_shape<T, false>(team, D, [&](auto t, auto it, auto whole) {
         constexpr int TEAM = decltype(t)::value, ITER = decltype(it)::value;
-        hipLaunchKernelGGL((norm_kernel<T, TEAM, ITER>),
+        constexpr bool FULL = decltype(whole)::value;
+        hipLaunchKernelGGL((norm_kernel<T, TEAM, ITER, FULL>),
                            dim3(uint32_t(blocks_for(TEAM, rows, kMaxBlocks))),
                            dim3(norm_block(TEAM)), 0, stream, x, residual, w, b, y, total, mean,
                            rstd, rows, int(D), eps);
@@ -403,10 +421,13 @@ hipError_t norm_grad(const T* dy, const T* x, const float* w, const float* mean,
                            x, mean, rstd, part, rows, D);
         e = hipGetLastError();
     } else {
-        P = blocks_for(team, rows, kGradBlocks);
-        e = with_shape<T, true>(team, D, [&](auto t, auto it) {
+        // four rows to a team where that leaves a workgroup to a CU
+        P = blocks_for(team, (rows + 3) / 4, kGradBlocks);
+        if (P < 256) P = blocks_for(team, rows, 256);
+        e = with_shape<T, true>(team, D, [&](auto t, auto it, auto whole) {
             constexpr int TEAM = decltype(t)::value, ITER = decltype(it)::value;
-            hipLaunchKernelGGL((norm_grad_kernel<T, TEAM, ITER>), dim3(uint32_t(P)),
+        constexpr bool FULL = decltype(whole)::value;
+            hipLaunchKernelGGL((norm_grad_kernel<T, TEAM, ITER, FULL>), dim3(uint32_t(P)),
                                dim3(norm_block(TEAM)), 0, stream, dy, x, w, mean, rstd, dtotal, dx,
                                part, rows, int(D));
             return hipGetLastError();

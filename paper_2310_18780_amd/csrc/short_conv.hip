@@ -24,9 +24,12 @@ namespace lh {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int64_t kThreads = 1 << 18;  // threads that fill the GPU: 4 wavefronts per SIMD
+constexpr int64_t kThreads = 1 << 16;  // one wavefront per SIMD  
 
-// Channels per thread: 16 bytes, half of that for long filters (registers).
+constexpr int kAhead = 4;  // steps whose inputs are in flight while as many are computed
+
+// Channels per thread: 16 bytes, half of that for long filters (registers); one where
+// the width is less.
 template <typename T, int K>
 constexpr int kChan = K <= 4 ? kVec<T> : kVec<T> / 2;
 
@@ -37,83 +40,130 @@ __device__ __forceinline__ int64_t length_of(const int* lengths, int64_t b, int6
     return n < 0 ? 0 : n < T ? n : T;
 }
 
-template <typename T, int K, bool SILU>
+// The values of a piece but the first `twice`.
+template <int V, typename T>
+__device__ __forceinline__ void put_from(T* p, const float (&v)[V], int twice)
+{
+    if (twice == 0) {
+        put<V>(p, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j >= twice) io_store(p + j, v[j]);
+    }
+}
+
+// The filter of V channels from c: w[k], K taps, and the bias.
+template <int V, int K>
+__device__ __forceinline__ void load_filter(const float* w, const float* bias, int64_t c,
+                                            float (&wv)[K][V], float (&bv)[V])
+{
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        bv[j] = bias ? bias[c + j] : 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) wv[k][j] = w[(c + j) * K + k];
+    }
+}
+
+// The input of step t of a row, or of the state where t < 0 (zero without one): where it
+// lies, and whether it is there.  No load is under a branch; one that is not there reads
+// another place and is replaced by zero.
+template <typename T, int K>
+__device__ __forceinline__ const T* place_of(int64_t t, const T* px, int64_t ld, const T* ps,
+                                             int64_t D, bool resume, bool* there)
+{
+    *there = t >= 0 || resume;
+    return t >= 0 ? px + t * ld : ps + (resume ? t + K - 1 : 0) * D;
+}
+
+template <typename T, int K, int V, bool SILU>
 __global__ __launch_bounds__(kBlock) void conv_kernel(
     const T* __restrict__ x, int64_t ld, const float* __restrict__ w,
-    const float* __restrict__ bias, const int* __restrict__ lengths, T* __restrict__ state,
-    bool resume, T* __restrict__ y, int64_t B, int64_t T_, int64_t D, int64_t run, int64_t runs)
+    const float* __restrict__ bias, const int* __restrict__ lengths, T* state, bool resume,
+    T* __restrict__ y, int64_t B, int64_t T_, int64_t D, int64_t run, int64_t runs)
 {
-    constexpr int V = kChan<T, K>;
     const int64_t cols = (D + V - 1) / V;
     const int64_t id = int64_t(blockIdx.x) * kBlock + threadIdx.x;
     const int64_t row = id / cols;
     if (row >= B * runs) return;
-    const int64_t c = (id - row * cols) * V, b = row / runs, r = row - b * runs;
-    const int n = int(D - c < V ? D - c : V);
+    // The last piece ends with the row.  The channels it shares with the one before are
+    // that one's to store (whose thread may have written their new state already).
+    const int64_t at = (id - row * cols) * V, c = at < D - V ? at : D - V;
+    const int twice = int(at - c);
+    const int64_t b = row / runs, r = row - b * runs;
     const int64_t len = length_of(lengths, b, T_);
-    const int64_t t0 = r * run, t1 = t0 + run < T_ ? t0 + run : T_;
+    const int64_t t0 = r * run, t1 = t0 + run < T_ ? t0 + run : T_, te = t1 < len ? t1 : len;
     const T* px = x + b * T_ * ld + c;
     T* py = y + b * T_ * D + c;
     T* ps = state + b * (K - 1) * D + c;
 
-    float win[K][V];  // win[k] = x_(t - K + 1 + k)
-#pragma unroll
-    for (int k = 0; k < K - 1; ++k) {
-        const int64_t t = t0 - (K - 1) + k;
-        if (t >= 0 && t < len)
-            load_some<V>(px + t * ld, n, win[k]);
-        else if (t < 0 && resume)
-            load_some<V>(ps + (t + K - 1) * D, n, win[k]);
-        else
-#pragma unroll
-            for (int j = 0; j < V; ++j) win[k][j] = 0.f;
-    }
-    if (r == 0) {
-        // The state after the row's last token.  Only this thread reads the old one
-        // (above, and here where the row is shorter than the state), so it may write.
-        float tail[K][V];
-#pragma unroll
-        for (int k = 0; k < K - 1; ++k) {
-            const int64_t t = len - (K - 1) + k;
-            if (t >= 0)
-                load_some<V>(px + t * ld, n, tail[k]);
-            else if (resume)
-                load_some<V>(ps + (t + K - 1) * D, n, tail[k]);
-            else
-#pragma unroll
-                for (int j = 0; j < V; ++j) tail[k][j] = 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < K - 1; ++k) store_some<V>(ps + k * D, n, tail[k]);
-    }
-    float wv[K][V], bv[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int64_t cj = c + (j < n ? j : 0);
-        bv[j] = bias ? bias[cj] : 0.f;
-#pragma unroll
-        for (int k = 0; k < K; ++k) wv[k][j] = w[cj * K + k];
-    }
-    const int64_t te = t1 < len ? t1 : len;
-    int64_t t = t0;
-    for (; t < te; ++t) {
-        load_some<V>(px + t * ld, n, win[K - 1]);
-        float o[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            o[j] = bv[j];
-#pragma unroll
-            for (int k = 0; k < K; ++k) o[j] = fmaf(wv[k][j], win[k][j], o[j]);
-            if constexpr (SILU) o[j] *= sigmoid(o[j]);
-        }
-        store_some<V>(py + t * D, n, o);
+    Raw<T, V> head[K], tail[K], next[kAhead];
+    bool in_head[K], in_tail[K];
+    if (t0 < te) {
 #pragma unroll
         for (int k = 0; k < K - 1; ++k)
+            head[k] = load_raw<V>(place_of<T, K>(t0 - (K - 1) + k, px, ld, ps, D, resume, &in_head[k]));
 #pragma unroll
-            for (int j = 0; j < V; ++j) win[k][j] = win[k + 1][j];
+        for (int i = 0; i < kAhead; ++i) next[i] = load_raw<V>(px + (t0 + i < te ? t0 + i : te - 1) * ld);
+    }
+    float wv[K][V], bv[V];
+    load_filter<V, K>(w, bias, c, wv, bv);
+    if (K > 1 && r == 0) {
+        // The state after the row's last token.  Only the threads of this piece read the
+        // old one, above and here where the row is shorter than the state.
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k)
+            tail[k] = load_raw<V>(place_of<T, K>(len - (K - 1) + k, px, ld, ps, D, resume, &in_tail[k]));
+    }
+    float win[K][V];  // win[k] = x_(t - K + 1 + k)
+    if (t0 < te) {
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k) {
+            expand<V, T>(head[k], win[k]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) win[k][j] = in_head[k] ? win[k][j] : 0.f;
+        }
+    }
+    if (K > 1 && r == 0) {
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k) {
+            float v[V];
+            expand<V, T>(tail[k], v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = in_tail[k] ? v[j] : 0.f;
+            put_from<V>(ps + k * D, v, twice);
+        }
+    }
+    // kAhead steps at a time, the next ones in flight
+    for (int64_t t = t0; t < te; t += kAhead) {
+        Raw<T, V> now[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            now[i] = next[i];
+            const int64_t ahead = t + kAhead + i;
+            next[i] = load_raw<V>(px + (ahead < te ? ahead : te - 1) * ld);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            expand<V, T>(now[i], win[K - 1]);
+            float o[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                o[j] = bv[j];
+#pragma unroll
+                for (int k = 0; k < K; ++k) o[j] = fmaf(wv[k][j], win[k][j], o[j]);
+                if constexpr (SILU) o[j] *= sigmoid(o[j]);
+            }
+            if (t + i < te) put_from<V>(py + (t + i) * D, o, twice);
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) win[k][j] = win[k + 1][j];
+        }
     }
     const float zero[V] = {};
-    for (; t < t1; ++t) store_some<V>(py + t * D, n, zero);
+    for (int64_t t = te > t0 ? te : t0; t < t1; ++t) put<V>(py + t * D, zero);
 }
 
 template <typename T, int K, bool SILU>
@@ -139,20 +189,22 @@ __global__ __launch_bounds__(kBlock) void conv_step_kernel(
 }
 
 // A workgroup: 64 pieces of channels x 4 runs, whose sums are added in LDS.
-template <typename T, int K, bool SILU>
+template <typename T, int K, int V, bool SILU>
 __global__ __launch_bounds__(kBlock) void conv_grad_kernel(
     const T* __restrict__ dy, const T* __restrict__ x, int64_t ld, const float* __restrict__ w,
     const float* __restrict__ bias, const int* __restrict__ lengths, T* __restrict__ dx,
     float* __restrict__ part, int64_t B, int64_t T_, int64_t D, int64_t run, int64_t runs)
 {
-    constexpr int V = kChan<T, K>;
     constexpr int kRuns = kBlock / kWave;
     __shared__ float sums[kRuns][V][kWave];
     const int64_t tiles = ((D + V - 1) / V + kWave - 1) / kWave;
     const int lane = threadIdx.x & (kWave - 1), sub = threadIdx.x / kWave;
     const int64_t tile = blockIdx.x % tiles, group = blockIdx.x / tiles;
     const int64_t row = group * kRuns + sub;
-    const int64_t c = (tile * kWave + lane) * V;
+    // (the last piece ends with the row: the channels it shares with the one before count
+    // there)
+    const int64_t at = (tile * kWave + lane) * V, c = at < D - V ? at : D - V;
+    const int twice = int(at - c < V ? at - c : V);
     float aw[K][V], ab[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
@@ -160,78 +212,97 @@ __global__ __launch_bounds__(kBlock) void conv_grad_kernel(
 #pragma unroll
         for (int k = 0; k < K; ++k) aw[k][j] = 0.f;
     }
-    if (row < B * runs && c < D) {
-        const int n = int(D - c < V ? D - c : V);
+    if (row < B * runs && at < D) {
         const int64_t b = row / runs, t0 = (row - b * runs) * run;
         const int64_t len = length_of(lengths, b, T_);
-        const int64_t t1 = t0 + run < T_ ? t0 + run : T_;
+        const int64_t t1 = t0 + run < T_ ? t0 + run : T_, te = t1 < len ? t1 : len;
         const T* px = x + b * T_ * ld + c;
         const T* pg = dy + b * T_ * D + c;
         T* pd = dx + b * T_ * D + c;
-        float wv[K][V], bv[V], win[K][V], g[K][V];
+        if (t0 < te) {
+            Raw<T, V> head[K], nx[kAhead], ng[kAhead];
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int64_t cj = c + (j < n ? j : 0);
-            bv[j] = bias ? bias[cj] : 0.f;
+            for (int k = 0; k < K - 1; ++k) {
+                const int64_t t = t0 - (K - 1) + k;
+                head[k] = load_raw<V>(px + (t > 0 ? t : 0) * ld);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t t = t0 + i < len ? t0 + i : len - 1;
+                nx[i] = load_raw<V>(px + t * ld);
+                ng[i] = load_raw<V>(pg + t * D);
+            }
+            float wv[K][V], bv[V], win[K][V], g[K][V];
+            load_filter<V, K>(w, bias, c, wv, bv);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                wv[k][j] = w[cj * K + k];
-                win[k][j] = g[k][j] = 0.f;
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < K - 1; ++k) {
-            const int64_t t = t0 - (K - 1) + k;
-            if (t >= 0 && t < len) load_some<V>(px + t * ld, n, win[k]);
-        }
-        // g[k] = g_(t - K + 1 + k); dx_(t - K + 1) leaves at step t.  The run's own steps
-        // feed dw and dbias, the K - 1 after it only its last dx.
-        const int64_t te = t1 < len ? t1 : len;
-        for (int64_t t = t0; t < te + K - 1; ++t) {
-            if (t < len) {
-                load_some<V>(px + t * ld, n, win[K - 1]);
-                load_some<V>(pg + t * D, n, g[K - 1]);
+                if (k < K - 1) expand<V, T>(head[k], win[k]);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    if constexpr (SILU) {
-                        float o = bv[j];
+                    if (k < K - 1) win[k][j] = t0 - (K - 1) + k >= 0 ? win[k][j] : 0.f;
+                    g[k][j] = 0.f;
+                }
+            }
+            // g[k] = g_(t - K + 1 + k); dx_(t - K + 1) leaves at step t.  The run's own
+            // steps feed dw and dbias, the K - 1 after it only its last dx.
+            for (int64_t t = t0; t < te + K - 1; t += kAhead) {
+                Raw<T, V> rx[kAhead], rg[kAhead];
 #pragma unroll
-                        for (int k = 0; k < K; ++k) o = fmaf(wv[k][j], win[k][j], o);
-                        const float p = sigmoid(o);
-                        g[K - 1][j] *= p * fmaf(o, 1.f - p, 1.f);
+                for (int i = 0; i < kAhead; ++i) {
+                    rx[i] = nx[i];
+                    rg[i] = ng[i];
+                    const int64_t ahead = t + kAhead + i < len ? t + kAhead + i : len - 1;
+                    nx[i] = load_raw<V>(px + ahead * ld);
+                    ng[i] = load_raw<V>(pg + ahead * D);
+                }
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int64_t now = t + i;
+                    expand<V, T>(rx[i], win[K - 1]);
+                    expand<V, T>(rg[i], g[K - 1]);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        if constexpr (SILU) {
+                            float o = bv[j];
+#pragma unroll
+                            for (int k = 0; k < K; ++k) o = fmaf(wv[k][j], win[k][j], o);
+                            const float p = sigmoid(o);
+                            g[K - 1][j] *= p * fmaf(o, 1.f - p, 1.f);
+                        }
+                        g[K - 1][j] = now < len ? g[K - 1][j] : 0.f;
                     }
-                    if (t < te) {
-                        ab[j] += g[K - 1][j];
+                    if (now < te) {
 #pragma unroll
-                        for (int k = 0; k < K; ++k)
-                            aw[k][j] = fmaf(g[K - 1][j], win[k][j], aw[k][j]);
+                        for (int j = 0; j < V; ++j) {
+                            ab[j] += g[K - 1][j];
+#pragma unroll
+                            for (int k = 0; k < K; ++k)
+                                aw[k][j] = fmaf(g[K - 1][j], win[k][j], aw[k][j]);
+                        }
                     }
-                }
-            } else {
+                    if (now - (K - 1) >= t0 && now - (K - 1) < te) {
+                        // w[K - 1] meets the output of its own step, w[0] the one K - 1 later
+                        float d[V];
 #pragma unroll
-                for (int j = 0; j < V; ++j) g[K - 1][j] = 0.f;
+                        for (int j = 0; j < V; ++j) {
+                            d[j] = 0.f;
+#pragma unroll
+                            for (int k = 0; k < K; ++k) d[j] = fmaf(wv[K - 1 - k][j], g[k][j], d[j]);
+                        }
+                        put<V>(pd + (now - (K - 1)) * D, d);
+                    }
+#pragma unroll
+                    for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) {
+                            win[k][j] = win[k + 1][j];
+                            g[k][j] = g[k + 1][j];
+                        }
+                }
             }
-            if (t - (K - 1) >= t0) {
-                // w[K - 1] meets the output of its own step, w[0] the one K - 1 later
-                float d[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    d[j] = 0.f;
-#pragma unroll
-                    for (int k = 0; k < K; ++k) d[j] = fmaf(wv[K - 1 - k][j], g[k][j], d[j]);
-                }
-                store_some<V>(pd + (t - (K - 1)) * D, n, d);
-            }
-#pragma unroll
-            for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    win[k][j] = win[k + 1][j];
-                    g[k][j] = g[k + 1][j];
-                }
         }
         const float zero[V] = {};
-        for (int64_t t = te > t0 ? te : t0; t < t1; ++t) store_some<V>(pd + t * D, n, zero);
+        for (int64_t t = te > t0 ? te : t0; t < t1; ++t) put<V>(pd + t * D, zero);
     }
     // partial row [D K | D] of this workgroup
     float* out = part + group * (K + 1) * D;
@@ -241,13 +312,11 @@ __global__ __launch_bounds__(kBlock) void conv_grad_kernel(
 #pragma unroll
         for (int j = 0; j < V; ++j) sums[sub][j][lane] = k < K ? aw[k < K ? k : 0][j] : ab[j];
         __syncthreads();
-        for (int i = threadIdx.x; i < V * kWave; i += kBlock) {
-            const int j = i / kWave, l = i % kWave;
-            const int64_t cj = (tile * kWave + l) * V + j;
+        for (int j = sub; j < V; j += kRuns) {  // (this thread's lane: the same piece)
             float s = 0.f;
 #pragma unroll
-            for (int q = 0; q < kRuns; ++q) s += sums[q][j][l];
-            if (cj < D) out[k < K ? cj * K + k : D * K + cj] = s;
+            for (int q = 0; q < kRuns; ++q) s += sums[q][j][lane];
+            if (at < D && j >= twice) out[k < K ? (c + j) * K + k : D * K + c + j] = s;
         }
     }
 }
@@ -302,7 +371,7 @@ int64_t short_conv_threads(int64_t B, int64_t T, int64_t D, int64_t K)
 {
     int64_t most = B * D;  // a step
     most = 16 * D * (K + 1) > most ? 16 * D * (K + 1) : most;  // column sums
-    for (int V : {2, 4, 8}) {
+    for (int V : {1, 2, 4, 8}) {
         const int64_t cols = (D + V - 1) / V, run = run_length(B, T, cols);
         const int64_t n = B * (T > 0 ? (T + run - 1) / run : 1) * cols + kBlock;
         most = n > most ? n : most;
@@ -324,12 +393,14 @@ hipError_t launch_short_conv(const void* x, int64_t ld, const float* w, const fl
         return with_taps(K, [&](auto taps) {
             constexpr int KK = decltype(taps)::value;
             constexpr int V = kChan<E, KK>;
-            const int64_t cols = (D + V - 1) / V;
+            const bool whole = D >= V;
+            const int64_t cols = whole ? (D + V - 1) / V : D;
             const int64_t run = run_length(B, T, cols);
             const int64_t runs = T > 0 ? (T + run - 1) / run : 1;
             const int64_t blocks = (B * runs * cols + kBlock - 1) / kBlock;
-            hipLaunchKernelGGL((conv_kernel<E, KK, S>), dim3(uint32_t(blocks)), dim3(kBlock), 0,
-                               stream, static_cast<const E*>(x), ld, w, bias, lengths,
+            const auto kernel = whole ? conv_kernel<E, KK, V, S> : conv_kernel<E, KK, 1, S>;
+            hipLaunchKernelGGL(kernel, dim3(uint32_t(blocks)), dim3(kBlock), 0, stream,
+                               static_cast<const E*>(x), ld, w, bias, lengths,
                                static_cast<E*>(state), resume, static_cast<E*>(y), B, T, D, run,
                                runs);
             return hipGetLastError();
@@ -357,9 +428,9 @@ hipError_t launch_short_conv_step(const void* x, int64_t ld, const float* w, con
 
 size_t short_conv_grad_workspace_bytes(int64_t B, int64_t T, int64_t D, int64_t K)
 {
-    // the wider of the two types' partial rows (pieces of 2 to 8 channels)
+    // the wider of the two types' partial rows (pieces of 1 to 8 channels)
     int64_t groups = 0;
-    for (int V : {2, 4, 8}) {
+    for (int V : {1, 2, 4, 8}) {
         const GradShape s = grad_shape(B, T, D, V);
         groups = s.groups > groups ? s.groups : groups;
     }
@@ -378,11 +449,13 @@ hipError_t launch_short_conv_grad(const void* dy, const void* x, int64_t ld, con
         constexpr bool S = decltype(act)::value;
         return with_taps(K, [&](auto taps) {
             constexpr int KK = decltype(taps)::value;
-            const GradShape s = grad_shape(B, T, D, kChan<E, KK>);
+            constexpr int V = kChan<E, KK>;
+            const GradShape s = grad_shape(B, T, D, D >= V ? V : 1);
             groups = s.groups;
             if (s.groups == 0) return hipSuccess;
-            hipLaunchKernelGGL((conv_grad_kernel<E, KK, S>), dim3(uint32_t(s.groups * s.tiles)),
-                               dim3(kBlock), 0, stream, static_cast<const E*>(dy),
+            const auto kernel = D >= V ? conv_grad_kernel<E, KK, V, S> : conv_grad_kernel<E, KK, 1, S>;
+            hipLaunchKernelGGL(kernel, dim3(uint32_t(s.groups * s.tiles)), dim3(kBlock), 0, stream,
+                               static_cast<const E*>(dy),
                                static_cast<const E*>(x), ld, w, bias, lengths,
                                static_cast<E*>(dx), part, B, T, D, s.run, s.runs);
             return hipGetLastError();
