@@ -505,38 +505,37 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _need_rows(t, name, dtype, lead, row) -> int:
-    """Checks ``t`` of shape ``lead + row`` (``lead``: ``(B, T)`` or ``(B,)``): contiguous
-    rows, a fixed distance apart; returns that distance in elements."""
-    # one test of all properties of a contiguous tensor, as in _need
-    if (isinstance(t, _torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == lead + row
-            and t.is_contiguous()):
-        return row[0] if len(row) == 1 else row[0] * row[1]
+def _need_rows(t, name, dtype, shape, lead, width) -> int:
+    """Checks ``t`` of this shape, the first ``lead`` axes (batch, or batch and time) of
+    which count rows of ``width`` contiguous elements, a fixed distance apart; returns
+    that distance in elements."""
+    # one test of all properties, as in _need
+    if isinstance(t, _torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == shape:
+        if t.is_contiguous():
+            return width
+        strides = t.stride()
+        n = 1
+        for i in range(len(shape) - 1, lead - 1, -1):
+            if strides[i] != n and shape[i] > 1:
+                raise ValueError(f"{name} must have contiguous rows")
+            n *= shape[i]
+        # (the stride of an axis of one says nothing)
+        if lead == 1 or shape[1] == 1:
+            ld = strides[0] if shape[0] > 1 else width
+        else:
+            ld = strides[1]
+            if shape[0] > 1 and strides[0] != shape[1] * ld:
+                raise ValueError(f"{name}: the rows of its batches must follow one another")
+        if ld < width:
+            raise ValueError(f"{name} must have rows that do not overlap")
+        return ld
     if not isinstance(t, _torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a HIP device, got {t.device}")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != lead + row:
-        raise ValueError(f"{name} must have shape {lead + row}, got {tuple(t.shape)}")
-    strides, width = t.stride(), 1
-    for n, s in zip(row[::-1], strides[::-1]):
-        if n > 1 and s != width:
-            raise ValueError(f"{name} must have contiguous rows")
-        width *= n
-    # (the stride of an axis of one says nothing)
-    if len(lead) == 1 or lead[1] == 1:
-        ld = strides[0] if lead[0] > 1 else width
-    else:
-        ld = strides[1]
-        if lead[0] > 1 and lead[1] > 0 and strides[0] != lead[1] * ld:
-            raise ValueError(f"{name}: the rows of its batches must follow one another")
-    if t.numel() == 0:
-        return width
-    if ld < width:
-        raise ValueError(f"{name} must have rows that do not overlap")
-    return ld
+    raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
 def _need_lengths(lengths, B):
@@ -611,7 +610,7 @@ def layer_norm_backward(dy, x, w, mean, rstd, dx, dw, db=None, dtotal=None, work
 def _conv_args(x, w, bias, lead):
     torch = _torch_loaded()
     D, K = w.shape
-    ld = _need_rows(x, "x", x.dtype, lead, (D,))
+    ld = _need_rows(x, "x", x.dtype, (*lead, D), len(lead), D)
     _need(w, "w", torch.float32, (D, K))
     if bias is not None:
         _need(bias, "bias", torch.float32, (D,))
@@ -669,32 +668,32 @@ def short_conv_backward(dy, x, w, bias, dx, dw, dbias=None, silu: bool = True, l
                                         dw.data_ptr(), _ptr(dbias), ws_ptr, ws_len, handle))
 
 
-def _selective_args(A, dt, Bm, Cm, u, h0, dt_bias, z, lengths, lead, suffix=""):
+def _selective_args(A, dt, Bm, Cm, u, h0, dt_bias, z, lengths, lead):
     torch = _torch_loaded()
     D, N = A.shape
     G = Bm.shape[-2]
-    s = _SelectiveInputs()
+    dtype, k = u.dtype, len(lead)
+    rows, sel = (*lead, D), (*lead, G, N)
     _need(A, "A", torch.float32, (D, N))
-    for name, t in (("dt_bias", dt_bias), ("h0", h0)):
-        if t is not None:
-            _need(t, name, torch.float32, (D,))
-            setattr(s, name, t.data_ptr())
-    dtype = u.dtype
-    s.io_dtype = _io_dtype(u)
-    s.A = A.data_ptr()
-    s.ld_dt = _need_rows(dt, "dt" + suffix, dtype, lead, (D,))
-    s.ld_u = _need_rows(u, "u" + suffix, dtype, lead, (D,))
-    s.ld_B = _need_rows(Bm, "Bm" + suffix, dtype, lead, (G, N))
-    s.ld_C = _need_rows(Cm, "Cm" + suffix, dtype, lead, (G, N))
-    s.dt, s.u, s.Bm, s.Cm = dt.data_ptr(), u.data_ptr(), Bm.data_ptr(), Cm.data_ptr()
+    ld_dt = _need_rows(dt, "dt", dtype, rows, k, D)
+    ld_u = _need_rows(u, "u", dtype, rows, k, D)
+    ld_B = _need_rows(Bm, "Bm", dtype, sel, k, G * N)
+    ld_C = _need_rows(Cm, "Cm", dtype, sel, k, G * N)
+    ld_z = pz = pb = ph = pl = None
     if z is not None:
-        s.ld_z = _need_rows(z, "z", dtype, lead, (D,))
-        s.z = z.data_ptr()
+        ld_z, pz = _need_rows(z, "z", dtype, rows, k, D), z.data_ptr()
+    if dt_bias is not None:
+        _need(dt_bias, "dt_bias", torch.float32, (D,))
+        pb = dt_bias.data_ptr()
+    if h0 is not None:
+        _need(h0, "h0", torch.float32, (D,))
+        ph = h0.data_ptr()
     if lengths is not None:
         _need_lengths(lengths, lead[0])
-        s.lengths = lengths.data_ptr()
-    s.B, s.T, s.D, s.N, s.G = lead[0], lead[1] if len(lead) > 1 else 1, D, N, G
-    return s
+        pl = lengths.data_ptr()
+    return _SelectiveInputs(A.data_ptr(), pb, ph, dt.data_ptr(), u.data_ptr(), pz, Bm.data_ptr(), Cm.data_ptr(), pl,
+                            ld_dt, ld_u, ld_z or 0, ld_B, ld_C, lead[0], lead[1] if k > 1 else 1, D, N, G,
+                            _io_dtype(u))
 
 
 def selective_workspace_bytes(B: int, T: int, D: int, N: int, G: int = 1) -> int:
@@ -723,7 +722,7 @@ def selective_step(A, dt_t, Bm_t, Cm_t, u_t, state, y_t, h0=None, dt_bias=None, 
     """One token per row (``lh_selective_step``): ``dt_t``, ``u_t``, ``z`` ``[B, D]``,
     ``Bm_t``, ``Cm_t`` ``[B, G, N]``, ``state`` in place."""
     B = u_t.shape[0]
-    s = _selective_args(A, dt_t, Bm_t, Cm_t, u_t, h0, dt_bias, z, None, (B,), "_t")
+    s = _selective_args(A, dt_t, Bm_t, Cm_t, u_t, h0, dt_bias, z, None, (B,))
     _need(state, "state", _torch.float32, (B, s.D, s.N))
     _need(y_t, "y_t", u_t.dtype, (B, s.D))
     _check(lib().lh_selective_step(ctypes.byref(s), state.data_ptr(), y_t.data_ptr(),

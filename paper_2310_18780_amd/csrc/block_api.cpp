@@ -96,11 +96,21 @@ lh_status check_buffers(const Arg (&ins)[I], const Arg (&outs)[O])
     }
     int dev = 0;
     if ((s = check_device(&dev)) != LH_OK) return s;
-    Buf seen{"", 0, 0};
+    // the allocations found accessible in this call: a framework's tensors share them
+    Buf seen[I + O] = {};
+    size_t n = 0;
+    auto accessible = [&](const Buf& b) {
+        for (size_t i = 0; i < n; ++i)
+            if (b.lo >= seen[i].lo && b.hi <= seen[i].hi) return LH_OK;
+        Buf found{"", 0, 0};
+        const lh_status r = check_accessible(b, dev, &found);
+        if (found.hi > found.lo) seen[n++] = found;
+        return r;
+    };
     for (const Arg& a : ins)
-        if ((s = check_accessible(a.b, dev, &seen)) != LH_OK) return s;
+        if ((s = accessible(a.b)) != LH_OK) return s;
     for (const Arg& a : outs)
-        if ((s = check_accessible(a.b, dev, &seen)) != LH_OK) return s;
+        if ((s = accessible(a.b)) != LH_OK) return s;
     return LH_OK;
 }
 

@@ -151,7 +151,9 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     // walked: zero times an infinite input is not zero.)
     auto walk = [&](auto count) {
         constexpr int CNT = decltype(count)::value;
-#pragma unroll
+        // (fewer steps unrolled where their values from LDS would not fit the registers)
+        constexpr int kUnroll = NS > 6 ? 2 : kSteps;
+#pragma unroll kUnroll
         for (int j = 0; j < kSteps; ++j) {
             const float2 d = step[j][lane];
             float acc = 0.f;
@@ -271,40 +273,46 @@ __global__ __launch_bounds__(256) void carry_kernel(const float* __restrict__ A,
     }
 }
 
-// Four states to a lane, LPR lanes to a (batch row, channel).
-template <typename T, int LPR>
-__global__ __launch_bounds__(256) void scan_step_kernel(Selective s, float* __restrict__ state,
-                                                        T* __restrict__ y)
+// V states to a lane (4, or 1 where there are fewer), LPR lanes to a (batch row,
+// channel).  A lane whose states would pass the row's end takes its last V: the first
+// `twice` of them are another lane's too, take no part in y, and are stored with the same
+// bits.  (The row's lanes are of one wavefront, which has read them all by then.)
+template <typename T, int V, int LPR>
+__global__ __launch_bounds__(256) void scan_step_kernel(Selective s, float* state, T* __restrict__ y)
 {
     const int sub = threadIdx.x % LPR;
     const int64_t row = (int64_t(blockIdx.x) * 256 + threadIdx.x) / LPR;
     if (row >= s.B * s.D) return;
     const int64_t b = row / s.D, c = row - b * s.D;
     const int64_t grp = c / (s.D / s.G);
-    const int n = sub * 4, cnt = s.N - n;
+    const int n = sub * V < s.N - V ? sub * V : s.N - V, twice = sub * V - n;
     float* px = state + row * s.N + n;
-    float x[4], A[4], Bv[4], Cv[4];
-    load_some<4>(px, cnt, x);
-    load_some<4>(s.A + c * s.N + n, cnt, A);
-    load_some<4>(static_cast<const T*>(s.Bm) + b * s.ld_b + grp * s.N + n, cnt, Bv);
-    load_some<4>(static_cast<const T*>(s.Cm) + b * s.ld_c + grp * s.N + n, cnt, Cv);
-    const float u = io_load(static_cast<const T*>(s.u) + b * s.ld_u + c);
-    const float delta = softplus(io_load(static_cast<const T*>(s.dt) + b * s.ld_dt + c) +
-                                 (s.dt_bias ? s.dt_bias[c] : 0.f));
-    const float du = delta * u;
+    const Raw<float, V> rx = load_raw<V>(px), rA = load_raw<V>(s.A + c * s.N + n);
+    const Raw<T, V> rB = load_raw<V>(static_cast<const T*>(s.Bm) + b * s.ld_b + grp * s.N + n);
+    const Raw<T, V> rC = load_raw<V>(static_cast<const T*>(s.Cm) + b * s.ld_c + grp * s.N + n);
+    const T ru = static_cast<const T*>(s.u)[b * s.ld_u + c];
+    const T rd = static_cast<const T*>(s.dt)[b * s.ld_dt + c];
+    const T rz = s.z ? static_cast<const T*>(s.z)[b * s.ld_z + c] : T();
+    const float bias = s.dt_bias ? s.dt_bias[c] : 0.f, h0 = s.h0 ? s.h0[c] : 0.f;
+    float x[V], A[V], Bv[V], Cv[V];
+    expand<V, float>(rx, x);
+    expand<V, float>(rA, A);
+    expand<V, T>(rB, Bv);
+    expand<V, T>(rC, Cv);
+    const float u = io_load(&ru), delta = softplus(io_load(&rd) + bias), du = delta * u;
     float o = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < V; ++i) {
         x[i] = fmaf(exp2_fast(delta * (A[i] * kLog2e)), x[i], du * Bv[i]);
-        if (i < cnt) o = fmaf(Cv[i], x[i], o);
+        if (i >= twice) o = fmaf(Cv[i], x[i], o);
     }
-    store_some<4>(px, cnt, x);
+    put<V>(px, x);
 #pragma unroll
     for (int off = 1; off < LPR; off *= 2) o += __shfl_xor(o, off, kWave);
     if (sub == 0) {
-        if (s.h0) o = fmaf(s.h0[c], u, o);
+        o = fmaf(h0, u, o);
         if (s.z) {
-            const float z = io_load(static_cast<const T*>(s.z) + b * s.ld_z + c);
+            const float z = io_load(&rz);
             o *= z * sigmoid(z);
         }
         io_store(y + row, o);
@@ -371,23 +379,23 @@ hipError_t scan(const Selective& s, float* state, bool resume, T* y, void* works
 template <typename T>
 hipError_t scan_step(const Selective& s, float* state, T* y, hipStream_t stream)
 {
+    const int V = s.N >= 4 ? 4 : 1;
     int lpr = 1;
-    while (lpr * 4 < s.N) lpr *= 2;
+    while (lpr * V < s.N) lpr *= 2;
     const dim3 grid(uint32_t((s.B * s.D * lpr + 255) / 256));
-    switch (lpr) {
-#define LH_STEP(l) \
-    case l: \
-        hipLaunchKernelGGL((scan_step_kernel<T, l>), grid, dim3(256), 0, stream, s, state, y); \
-        break
-        LH_STEP(1);
-        LH_STEP(2);
-        LH_STEP(4);
-        LH_STEP(8);
-        LH_STEP(16);
-        default:
-            LH_STEP(32);
+#define LH_STEP(v, l) \
+    if (V == v && lpr == l) \
+    hipLaunchKernelGGL((scan_step_kernel<T, v, l>), grid, dim3(256), 0, stream, s, state, y)
+    LH_STEP(1, 1);
+    LH_STEP(1, 2);
+    LH_STEP(1, 4);
+    LH_STEP(4, 1);
+    LH_STEP(4, 2);
+    LH_STEP(4, 4);
+    LH_STEP(4, 8);
+    LH_STEP(4, 16);
+    LH_STEP(4, 32);
 #undef LH_STEP
-    }
     return hipGetLastError();
 }
 
