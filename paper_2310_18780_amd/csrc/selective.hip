@@ -84,17 +84,24 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     const float bias = s.dt_bias ? s.dt_bias[c] : 0.f;
     const float h0 = OUT && s.h0 ? s.h0[c] : 0.f;
 
+    // (slots past N load the last state and become zeros, so that no load waits alone)
     float A2[NS], x[NS];
+    const int64_t lastn = N - 1;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-        A2[i] = i < real ? s.A[c * N + n0 + i] * kLog2e : 0.f;
+        A2[i] = s.A[c * N + (n0 + i < N ? n0 + i : lastn)];
         x[i] = 0.f;
-        if (OUT && i < real) {
-            if (nchunks > 1)
-                x[i] = xs[((b * nchunks + k) * N + n0 + i) * s.D + c];
-            else if (resume)
-                x[i] = state[(b * s.D + c) * N + n0 + i];
-        }
+    }
+    if (OUT && (nchunks > 1 || resume)) {
+        const float* from = nchunks > 1 ? xs + (b * nchunks + k) * N * s.D + c : state + (b * s.D + c) * N;
+        const int64_t stride = nchunks > 1 ? s.D : 1;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) x[i] = from[(n0 + i < N ? n0 + i : lastn) * stride];
+    }
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        A2[i] = i < real ? A2[i] * kLog2e : 0.f;
+        x[i] = i < real ? x[i] : 0.f;
     }
     float total = 0.f;  // sum of the steps
 

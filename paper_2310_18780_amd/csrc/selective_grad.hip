@@ -157,10 +157,12 @@ __global__ __launch_bounds__(kWave* S) void grad_ends_kernel(Selective s, Select
     float A2[NS], x[NS], dec[NS], r[NS], total = 0.f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-        A2[i] = i < p.real ? s.A[p.c * s.N + p.n0 + i] * kLog2e : 0.f;
+        A2[i] = s.A[p.c * s.N + (i < p.real ? p.n0 + i : s.N - 1)];
         x[i] = r[i] = 0.f;
         dec[i] = 1.f;
     }
+#pragma unroll
+    for (int i = 0; i < NS; ++i) A2[i] = i < p.real ? A2[i] * kLog2e : 0.f;
 #pragma unroll 4
     for (int j = 0; j < chunk_steps(NS); ++j) {
         const float delta = m.delta[j][p.lane], du = m.du[j][p.lane], d = m.d[j][p.lane];
@@ -294,12 +296,20 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
     float A[NS], A2[NS], x[NS], G[NS], dA[NS];
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-        A[i] = i < p.real ? s.A[p.c * s.N + p.n0 + i] : 0.f;
-        A2[i] = A[i] * kLog2e;
-        const int64_t at = ((p.b * nchunks + p.k) * s.N + p.n0 + i) * s.D + p.c;
-        x[i] = i < p.real ? w.xs[at] : 0.f;
-        G[i] = i < p.real ? w.gs[at] : 0.f;
+        // (slots past N load the last state and become zeros, so that no load waits alone)
+        const int n = i < p.real ? p.n0 + i : s.N - 1;
+        A[i] = s.A[p.c * s.N + n];
+        const int64_t at = ((p.b * nchunks + p.k) * s.N + n) * s.D + p.c;
+        x[i] = w.xs[at];
+        G[i] = w.gs[at];
         dA[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        A[i] = i < p.real ? A[i] : 0.f;
+        x[i] = i < p.real ? x[i] : 0.f;
+        G[i] = i < p.real ? G[i] : 0.f;
+        A2[i] = A[i] * kLog2e;
     }
     const float bias = s.dt_bias ? s.dt_bias[p.c] : 0.f, h0 = s.h0 ? s.h0[p.c] : 0.f;
     float dh0 = 0.f, dbias = 0.f;
