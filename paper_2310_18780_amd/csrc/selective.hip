@@ -27,6 +27,10 @@ namespace lh {
 namespace {
 
 constexpr int kSteps = 16;  // steps of a tile
+// Up to this many chunks a launch for the carry costs more than carrying in every chunk
+// (1 row of 512 steps, D = 768: 18.9 us against 21.1; of 2048 steps, 64 chunks, 69.7
+// against 52.5).
+constexpr int64_t kFewChunks = 16;
 
 // f with n as a constant, 0 <= n <= MOST (n < 0 is 0).
 template <int MOST, typename F>
@@ -44,8 +48,9 @@ __device__ __forceinline__ void with_count(int n, const F& f)
 
 template <typename T, int NS, int S, bool OUT, bool GATE>
 __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chunk,
-                                                        int64_t nchunks, float* xs, float* sums,
-                                                        float* state, bool resume, T* y)
+                                                        int64_t nchunks, bool carried,
+                                                        float* xs, float* sums, float* state,
+                                                        bool resume, T* y)
 {
     constexpr int R = kSteps / S;    // rows per wavefront
     constexpr int W = OUT ? 2 : 1;   // B (and C)
@@ -60,7 +65,8 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     const int N = s.N;
     const int64_t Dg = s.D / s.G, per = group_tiles(s.D, s.G), tiles = per * s.G;
     const int64_t tile = blockIdx.x % tiles, rest = blockIdx.x / tiles;
-    const int64_t k = rest % nchunks, b = rest / nchunks;
+    // (nobody needs the last chunk's end state from zero)
+    const int64_t chunks = OUT ? nchunks : nchunks - 1, k = rest % chunks, b = rest / chunks;
     const int64_t grp = tile / per, c0 = grp * Dg + (tile % per) * kWave;  // the tile's first channel
     const int width = int((grp + 1) * Dg - c0 < kWave ? (grp + 1) * Dg - c0 : kWave);
     // Lanes past the group compute its last channel and store the same bits as its own
@@ -92,7 +98,7 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
         A2[i] = s.A[c * N + (n0 + i < N ? n0 + i : lastn)];
         x[i] = 0.f;
     }
-    if (OUT && (nchunks > 1 || resume)) {
+    if (OUT && (nchunks > 1 ? carried : resume)) {
         const float* from = nchunks > 1 ? xs + (b * nchunks + k) * N * s.D + c : state + (b * s.D + c) * N;
         const int64_t stride = nchunks > 1 ? s.D : 1;
 #pragma unroll
@@ -102,6 +108,29 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     for (int i = 0; i < NS; ++i) {
         A2[i] = i < real ? A2[i] * kLog2e : 0.f;
         x[i] = i < real ? x[i] : 0.f;
+    }
+    if (OUT && nchunks > 1 && !carried) {
+        // few chunks, from zero: the end states before this chunk are carried here
+        const float* end = xs + b * nchunks * N * s.D + c;
+        const float* sum = sums + b * nchunks * s.D + c;
+        constexpr int U = 8;
+        for (int64_t j0 = 0; j0 < k; j0 += U) {
+            float e[U][NS], d[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const int64_t at = j0 + j < k ? j0 + j : k - 1;
+                d[j] = sum[at * s.D];
+#pragma unroll
+                for (int i = 0; i < NS; ++i)
+                    e[j][i] = end[(at * N + (n0 + i < N ? n0 + i : lastn)) * s.D];
+            }
+#pragma unroll
+            for (int j = 0; j < U; ++j)
+                if (j0 + j < k) {
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) x[i] = fmaf(exp2_fast(A2[i] * d[j]), x[i], e[j][i]);
+                }
+        }
     }
     float total = 0.f;  // sum of the steps
 
@@ -267,7 +296,7 @@ __global__ __launch_bounds__(256) void carry_kernel(const float* __restrict__ A,
         float end[U], a[U];
 #pragma unroll
         for (int i = 0; i < U; ++i)
-            if (k + i < nchunks) {
+            if (k + i < nchunks - 1) {
                 end[i] = px[(k + i) * N * D];
                 a[i] = ps[(k + i) * D];
             }
@@ -275,7 +304,7 @@ __global__ __launch_bounds__(256) void carry_kernel(const float* __restrict__ A,
         for (int i = 0; i < U; ++i)
             if (k + i < nchunks) {
                 px[(k + i) * N * D] = x;
-                x = fmaf(exp2_fast(A2 * a[i]), x, end[i]);
+                if (k + i < nchunks - 1) x = fmaf(exp2_fast(A2 * a[i]), x, end[i]);
             }
     }
 }
@@ -365,20 +394,26 @@ hipError_t scan(const Selective& s, float* state, bool resume, T* y, void* works
     float* sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.off_sums);
     return with_split(p.ns, p.waves, [&](auto ns, auto waves) {
         constexpr int NS = decltype(ns)::value, S = decltype(waves)::value;
+        // (a chunk carries the end states before it by itself where they are few and nothing
+        // else is written that another chunk reads)
+        const bool carried = p.nchunks > kFewChunks || resume;
         if (p.nchunks > 1) {
-            hipLaunchKernelGGL((scan_kernel<T, NS, S, false, false>), dim3(uint32_t(blocks)),
-                               dim3(kWave * S), 0, stream, s, p.chunk, p.nchunks, xs, sums, state,
-                               resume, y);
+            hipLaunchKernelGGL((scan_kernel<T, NS, S, false, false>),
+                               dim3(uint32_t(blocks / p.nchunks * (p.nchunks - 1))),
+                               dim3(kWave * S), 0, stream, s, p.chunk, p.nchunks, carried, xs, sums,
+                               state, resume, y);
             hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
-            hipLaunchKernelGGL(carry_kernel, dim3(uint32_t((s.B * s.D * s.N + 255) / 256)),
-                               dim3(256), 0, stream, s.A, sums, xs, state, resume, s.B, s.D, s.N,
-                               p.nchunks);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
+            if (carried) {
+                hipLaunchKernelGGL(carry_kernel, dim3(uint32_t((s.B * s.D * s.N + 255) / 256)),
+                                   dim3(256), 0, stream, s.A, sums, xs, state, resume, s.B, s.D,
+                                   s.N, p.nchunks);
+                if ((e = hipGetLastError()) != hipSuccess) return e;
+            }
         }
         const auto last = s.z ? scan_kernel<T, NS, S, true, true> : scan_kernel<T, NS, S, true, false>;
         hipLaunchKernelGGL(last, dim3(uint32_t(blocks)), dim3(kWave * S), 0, stream, s, p.chunk,
-                           p.nchunks, xs, sums, state, resume, y);
+                           p.nchunks, carried, xs, sums, state, resume, y);
         return hipGetLastError();
     });
 }
@@ -414,7 +449,7 @@ SelectivePlan selective_plan(int64_t B, int64_t T, int64_t D, int N, int G)
     const int64_t tiles = B * group_tiles(D, G) * G;
     // One pass takes about 6 us and 0.1 us a step while the tiles leave the SIMDs waiting
     // (8 wavefronts to a tile, up to 270 tiles; then in proportion); chunks take 14 us for
-    // three launches and, with the SIMDs full, 0.45 ns a step and tile at 16 states.
+    // two or three launches and, with the SIMDs full, 0.45 ns a step and tile at 16 states.
     // (T = 2048, D = 2048, 16 states, one pass and chunks: 4 rows 199 and 133 us, 6 rows
     // 200 and 194, 8 rows 199 and 232; 4 rows of 128 steps 18 and 25 us, 1 row of 256 steps
     // 30 and 22 us.)
