@@ -8,19 +8,31 @@
 //
 // Prompts.  A lane is a channel, so u, dt, z and y are read and written in whole
 // lines, once.  The states of a 64-channel tile are split over the wavefronts of a
-// workgroup, ns to a lane in registers; a tile of 16 steps passes through LDS: its
+// workgroup, a few to a lane in registers; a tile of 16 steps passes through LDS: its
 // wavefronts form the steps (delta, delta u) of some rows each, walk all 16 rows for
-// their own states, and add the wavefronts' parts of y for some rows each.  Per state
-// and step that is two products, two multiply-adds and an exponential; the
-// exponential (8 cycles) and the four (4 cycles each) are what bounds the kernel.
+// their own states, and add the wavefronts' parts of y for some rows each.  The loads of
+// the next tile are in flight while one is walked.
+//
+// Bound by the VALU: per state and step two products, two multiply-adds (4 cycles each)
+// and an exponential (8 cycles), beside about 38 instructions a channel and step for
+// softplus, silu, the sum of the parts and conversions.  16 x 4096 x 2048 bfloat16 with 16
+// states: 568 us (1.9 TB/s; vector issue 0.73 of the time at 2.4 GHz, and the clock is
+// nearer 2.0 under this load).  What brought it there from 2047 us: loads not converted
+// where they are issued (784), 32-bit byte offsets from a uniform row and no branch for
+// the row's end inside a tile (629), twice the wavefronts with half the states (570).
+// Taken back: two tiles' buffers and one barrier a tile (LDS leaves fewer workgroups,
+// 1.4 times the time), values read from LDS a group of steps ahead (1.1 times), the rank-1
+// update as a 4x4x1 matrix instruction (its moves cost more than the products it saves).
 //
 // Where batch rows and tiles leave SIMDs idle the prompt is cut into chunks: a first
 // pass forms each chunk's end state from zero and its sum of steps (a chunk's decay is
 // e^(A sum delta), one exponential), a carry turns end states into entry states, and
-// the output pass starts every chunk from its own.
+// the output pass starts every chunk from its own: 0.83 times the output pass's work
+// again, for all SIMDs (1 x 65536 x 1024 float32: 479 us, the passes 197 and 264).
 //
 // Single tokens: four states of a (batch row, channel) to a lane, y summed over the
-// row's lanes; bound by the state, read once and written once.
+// row's lanes; bound by the state, read once and written once (64 x 2048, 16 states, 18
+// MB: 5.5 us in a graph, and 9 us a call from the host).
 #include "selective.hpp"
 
 namespace lh {

@@ -10,12 +10,15 @@
 // A thread holds 16 bytes of channels and walks a run of time steps with the K - 1
 // inputs before it in registers, so each input is loaded once, but for the K - 1 at
 // the start of a run, which the run before it has just loaded.  Runs are as long as
-// leaves the GPU enough threads.
+// leaves the GPU a wavefront per SIMD, and the inputs of the next four steps are in
+// flight while four are computed: 64 x 4096 x 2048 bfloat16 in 426 us (5.0 TB/s, the
+// rate of a copy; 463 us with each step's input waited for).
 //
 // The gradient walks the same way: o_t and g_t at the front, dx K - 1 steps behind.
 // A run's sums for dw and dbias stay in registers; the workgroup's runs over the
 // same channels are added in LDS, and a second launch adds the workgroups' rows in a
-// fixed order.
+// fixed order (16 x 2048 x 768 float32, rows 2 x 768 apart: 71 us for 302 MB, 84 us
+// without the inputs ahead; 64 x 2048 x 2048 bfloat16 361 us, 4.5 TB/s, against 554).
 #include "short_conv.hpp"
 
 #include "block_ops.hpp"
