@@ -418,7 +418,9 @@ hipError_t norm_grad(const T* dy, const T* x, const float* w, const float* mean,
     int64_t P;
     hipError_t e;
     if (team == 0) {
-        P = rows < 16 ? rows : 16;
+        P = 2048 / ((D + 255) / 256);  // eight workgroups to a CU
+        P = P < 16 ? 16 : P > kGradBlocks ? kGradBlocks : P;
+        P = P < rows ? P : rows;
         hipLaunchKernelGGL((norm_grad_wide_kernel<T>),
                            dim3(uint32_t(rows < kMaxBlocks ? rows : kMaxBlocks)), dim3(1024), 0,
                            stream, dy, x, w, mean, rstd, dtotal, dx, rows, D);

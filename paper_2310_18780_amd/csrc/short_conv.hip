@@ -113,8 +113,8 @@ __global__ __launch_bounds__(kBlock) void conv_kernel(
     float wv[K][V], bv[V];
     load_filter<V, K>(w, bias, c, wv, bv);
     if (K > 1 && r == 0) {
-        // The state after the row's last token.  Only the threads of this piece read the
-        // old one, above and here where the row is shorter than the state.
+        // The state after the row's last token.  Only the first runs of a row read the old
+        // one, above and here where the row is shorter than the state.
 #pragma unroll
         for (int k = 0; k < K - 1; ++k)
             tail[k] = load_raw<V>(place_of<T, K>(len - (K - 1) + k, px, ld, ps, D, resume, &in_tail[k]));
@@ -324,22 +324,25 @@ __global__ __launch_bounds__(kBlock) void conv_grad_kernel(
     }
 }
 
-// Time steps per run: as many as leave kThreads threads, 4 to 64.
-int64_t run_length(int64_t B, int64_t T, int64_t cols)
+// Time steps per run: as many as leave kThreads threads, 4 to 64, and not fewer than the
+// inputs before a run: only the first run of a row may reach back to the state, which its
+// thread replaces.
+int64_t run_length(int64_t B, int64_t T, int64_t cols, int64_t K)
 {
+    const int64_t least = K <= 5 ? 4 : 8;
     int64_t run = 64;
-    while (run > 4 && B * ((T + run - 1) / run) * cols < kThreads) run /= 2;
+    while (run > least && B * ((T + run - 1) / run) * cols < kThreads) run /= 2;
     return run;
 }
 
 struct GradShape {
     int64_t run, runs, groups, tiles;
 };
-GradShape grad_shape(int64_t B, int64_t T, int64_t D, int V)
+GradShape grad_shape(int64_t B, int64_t T, int64_t D, int64_t K, int V)
 {
     GradShape s;
     const int64_t cols = (D + V - 1) / V;
-    s.run = run_length(B, T, cols);
+    s.run = run_length(B, T, cols, K);
     s.runs = (T + s.run - 1) / s.run;
     s.groups = (B * s.runs + 3) / 4;
     s.tiles = (cols + kWave - 1) / kWave;
@@ -375,10 +378,10 @@ int64_t short_conv_threads(int64_t B, int64_t T, int64_t D, int64_t K)
     int64_t most = B * D;  // a step
     most = 16 * D * (K + 1) > most ? 16 * D * (K + 1) : most;  // column sums
     for (int V : {1, 2, 4, 8}) {
-        const int64_t cols = (D + V - 1) / V, run = run_length(B, T, cols);
+        const int64_t cols = (D + V - 1) / V, run = run_length(B, T, cols, K);
         const int64_t n = B * (T > 0 ? (T + run - 1) / run : 1) * cols + kBlock;
         most = n > most ? n : most;
-        const GradShape s = grad_shape(B, T, D, V);
+        const GradShape s = grad_shape(B, T, D, K, V);
         const int64_t m = s.groups * s.tiles * kBlock;
         most = m > most ? m : most;
     }
@@ -398,7 +401,7 @@ hipError_t launch_short_conv(const void* x, int64_t ld, const float* w, const fl
             constexpr int V = kChan<E, KK>;
             const bool whole = D >= V;
             const int64_t cols = whole ? (D + V - 1) / V : D;
-            const int64_t run = run_length(B, T, cols);
+            const int64_t run = run_length(B, T, cols, K);
             const int64_t runs = T > 0 ? (T + run - 1) / run : 1;
             const int64_t blocks = (B * runs * cols + kBlock - 1) / kBlock;
             const auto kernel = whole ? conv_kernel<E, KK, V, S> : conv_kernel<E, KK, 1, S>;
@@ -434,7 +437,7 @@ size_t short_conv_grad_workspace_bytes(int64_t B, int64_t T, int64_t D, int64_t 
     // the wider of the two types' partial rows (pieces of 1 to 8 channels)
     int64_t groups = 0;
     for (int V : {1, 2, 4, 8}) {
-        const GradShape s = grad_shape(B, T, D, V);
+        const GradShape s = grad_shape(B, T, D, K, V);
         groups = s.groups > groups ? s.groups : groups;
     }
     return sizeof(float) * size_t(groups) * (K + 1) * D;
@@ -453,7 +456,7 @@ hipError_t launch_short_conv_grad(const void* dy, const void* x, int64_t ld, con
         return with_taps(K, [&](auto taps) {
             constexpr int KK = decltype(taps)::value;
             constexpr int V = kChan<E, KK>;
-            const GradShape s = grad_shape(B, T, D, D >= V ? V : 1);
+            const GradShape s = grad_shape(B, T, D, K, D >= V ? V : 1);
             groups = s.groups;
             if (s.groups == 0) return hipSuccess;
             const auto kernel = D >= V ? conv_grad_kernel<E, KK, V, S> : conv_grad_kernel<E, KK, 1, S>;

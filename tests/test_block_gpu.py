@@ -183,6 +183,23 @@ def test_short_conv_prefill(case, resume, silu, io):
     assert np.array_equal(np64(state), sref)
 
 
+@pytest.mark.parametrize("K", [4, 5, 6, 8])
+def test_short_conv_resumes_with_long_filters_on_many_rows(K):
+    """The inputs before the first tokens come from the state as it was, whichever part of
+    a row runs first: few threads (the shortest runs) over many rows, against one row each."""
+    B, T, D = 64, 23, 24
+    r = gen(K + 50)
+    x, w = dev(r.normal(size=(B, T, D))), dev(r.normal(size=(D, K)))
+    old = dev(r.normal(size=(B, K - 1, D)))
+    ref, sref = ob.short_conv(np64(x), np64(w), None, False, state=np64(old))
+    mag, _ = ob.short_conv(np64(x), np64(w), None, False, state=np64(old), magnitude=True)
+    for _ in range(5):
+        state, y = old.clone(), nan_like((B, T, D))
+        lh.short_conv_prefill(x, w, None, state, y, silu=False, resume=True)
+        check(y, ref, mag, K + 16, name="y")
+        assert np.array_equal(np64(state), sref)
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("K", [1, 2, 4, 8])
 def test_short_conv_steps_continue_a_prefill(K, io):
