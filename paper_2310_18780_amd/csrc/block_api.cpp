@@ -120,7 +120,7 @@ lh_status check_norm_sizes(int64_t rows, int64_t D)
     if ((s = check_at_least("rows", rows, 0)) || (s = check_at_least("D", D, 1)) ||
         (s = check_product("rows, D", rows, D)))
         return s;
-    return check_threads(32 * D + 1024);  // column sums
+    return check_threads(2 * 32 * D + 1024);  // column sums
 }
 
 lh_status check_conv_sizes(int64_t B, int64_t T, int64_t D, int64_t K)

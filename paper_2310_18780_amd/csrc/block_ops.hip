@@ -5,17 +5,20 @@
 namespace lh {
 namespace {
 
-constexpr int kSlices = 16;  // rows are summed in 16 interleaved slices, then across them
+// A workgroup sums 32 columns (a line of a row), the rows in 32 interleaved slices, then
+// across those.  (64 columns in 16 slices leave half the workgroups: 1024 rows of 4096
+// columns 7 us.)
+constexpr int kCols = 32, kSlices = 32;
 
-__global__ __launch_bounds__(kWave* kSlices) void column_sum_kernel(
+__global__ __launch_bounds__(kCols* kSlices) void column_sum_kernel(
     const float* __restrict__ part, int64_t P, int64_t n0, float* out0, int64_t n1, float* out1,
     int64_t n2, float* out2)
 {
-    __shared__ float red[kSlices][kWave];
-    const int lane = threadIdx.x & (kWave - 1);
-    const int slice = threadIdx.x / kWave;
+    __shared__ float red[kSlices][kCols];
+    const int lane = threadIdx.x % kCols;
+    const int slice = threadIdx.x / kCols;
     const int64_t Q = n0 + n1 + n2;
-    const int64_t q = int64_t(blockIdx.x) * kWave + lane;
+    const int64_t q = int64_t(blockIdx.x) * kCols + lane;
     float acc = 0.f;
     if (q < Q) {
         const float* p = part + q;
@@ -47,8 +50,8 @@ __global__ __launch_bounds__(kWave* kSlices) void column_sum_kernel(
 hipError_t launch_column_sum(const float* part, int64_t P, int64_t n0, float* out0, int64_t n1,
                              float* out1, int64_t n2, float* out2, hipStream_t stream)
 {
-    const int64_t blocks = (n0 + n1 + n2 + kWave - 1) / kWave;
-    hipLaunchKernelGGL(column_sum_kernel, dim3(uint32_t(blocks)), dim3(kWave * kSlices), 0, stream,
+    const int64_t blocks = (n0 + n1 + n2 + kCols - 1) / kCols;
+    hipLaunchKernelGGL(column_sum_kernel, dim3(uint32_t(blocks)), dim3(kCols * kSlices), 0, stream,
                        part, P, n0, out0, n1, out1, n2, out2);
     return hipGetLastError();
 }

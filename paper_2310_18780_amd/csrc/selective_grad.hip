@@ -25,8 +25,8 @@
 //
 // Bound by the VALU: per state and step 7 instructions (one an exponential) in the first
 // pass and 28 in the main one (two exponentials, 5 of them folds).  4 x 4096 x 2048
-// bfloat16 with 16 states: 824 us (225 the first pass, 30 the carry, 615 the main pass, 19
-// and 9 the sums; vector issue 0.70 of both passes at 2.4 GHz).  With each load of a chunk
+// bfloat16 with 16 states: 820 us (225 the first pass, 30 the carry, 600 the main pass, 19
+// and 9 the sums, traced; vector issue 0.70 of both passes at 2.4 GHz).  With each load of a chunk
 // waited for in turn it took 1425 us.
 #include "selective.hpp"
 
@@ -244,20 +244,20 @@ __device__ __forceinline__ float fold(float a, float b, int lane)
                                                                        __float_as_uint(b), false, false));
         return __uint_as_float(r[0]) + __uint_as_float(r[1]);
     } else {
+        // (bound_ctrl lets the compiler take the permuted operand into the addition)
         const bool hi = lane & BIT;
         const float keep = hi ? b : a, send = hi ? a : b;
         const int v = __builtin_bit_cast(int, send);
         int q;
         if constexpr (BIT == 8)
-            q = __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, false);  // row_ror:8
+            q = __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, true);  // row_ror:8
         else if constexpr (BIT == 4)
-            // lane ^ 7 within 8, then ^ 3 within 4: lane ^ 4
-            q = __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, false), 0x1B,
-                                         0xF, 0xF, false);
+            // lane ^ 7 within 8: the lower bits' folds come after and sum over them anyway
+            q = __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true);
         else if constexpr (BIT == 2)
-            q = __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, false);  // quad_perm [2,3,0,1]
+            q = __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true);  // quad_perm [2,3,0,1]
         else
-            q = __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, false);  // quad_perm [1,0,3,2]
+            q = __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true);  // quad_perm [1,0,3,2]
         return keep + __builtin_bit_cast(float, q);
     }
 }
@@ -616,7 +616,7 @@ int64_t selective_threads(int64_t B, int64_t T, int64_t D, int N, int G, bool gr
     if (grad) {
         at_least(B * grad_chunks(T, N) * tiles * (N <= 16 ? 256 : N <= 64 ? 512 : 1024));
         at_least(B * T * G * 2 * N);
-        at_least(16 * D * (N + 2));  // column sums
+        at_least(32 * D * (N + 2));  // column sums
     }
     return most + 1024;
 }

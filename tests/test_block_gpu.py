@@ -299,6 +299,28 @@ def test_selective_prefill(case, gate, resume, io):
     check(state, xref, xmag, k, name="state")
 
 
+# prompts that are cut into more chunks than carry by themselves, and into a few
+LONG = [(1, 1200, 20, 16, 1, None), (2, 1100, 10, 8, 1, [1100, 530]), (1, 560, 70, 4, 2, None), (1, 1030, 6, 33, 3, [1017])]
+
+
+@pytest.mark.parametrize("resume", [False, True])
+@pytest.mark.parametrize("case", LONG, ids=str)
+def test_selective_prefill_in_chunks(case, resume):
+    B, T, D, N, G, lengths = case
+    assert lh.selective_workspace_bytes(B, T, D, N, G) > 0
+    c = scan_case(case, "f32", seed=3)
+    state = dev(gen(T).normal(size=(B, D, N))) if resume else nan_like((B, D, N))
+    args = dict(host(c), state=np64(state) if resume else None, lengths=lengths)
+    ref, xref = ob.selective(**args)
+    mag, xmag = ob.selective(**args, magnitude=True)
+    if lengths is not None:
+        poison(c, lengths, ("dt", "Bm", "Cm", "u", "z"))
+    y = nan_like((B, T, D))
+    lh.selective_prefill(state=state, y=y, lengths=device_lengths(lengths), resume=resume, **c)
+    check(y, ref, mag, 3 * T + N + 64, name="y")
+    check(state, xref, xmag, 3 * T + N + 64, name="state")
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("N", [1, 3, 4, 6, 8, 13, 16, 31, 32, 64, 100, 128])
 def test_selective_steps(N, io):
