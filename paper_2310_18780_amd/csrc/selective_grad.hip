@@ -25,7 +25,7 @@
 //
 // Bound by the VALU: per state and step 7 instructions (one an exponential) in the first
 // pass and 28 in the main one (two exponentials, 5 of them folds).  4 x 4096 x 2048
-// bfloat16 with 16 states: 820 us (225 the first pass, 30 the carry, 600 the main pass, 19
+// bfloat16 with 16 states: 820 us (225 the first pass, 30 the carry, 615 the main pass, 19
 // and 9 the sums, traced; vector issue 0.70 of both passes at 2.4 GHz).  With each load of a chunk
 // waited for in turn it took 1425 us.
 #include "selective.hpp"
