@@ -430,8 +430,9 @@ hipError_t norm_grad(const T* dy, const T* x, const float* w, const float* mean,
                            x, mean, rstd, part, rows, D);
         e = hipGetLastError();
     } else {
-        // four rows to a team where that leaves a workgroup to a CU
-        P = blocks_for(team, (rows + 3) / 4, kGradBlocks);
+        // Eight rows to a team, since a partial row costs about as much as two (4096 rows of
+        // 2048 bfloat16: 21 us, with four 26), where that leaves a workgroup to a CU.
+        P = blocks_for(team, (rows + 7) / 8, kGradBlocks);
         if (P < 256) P = blocks_for(team, rows, 256);
         e = with_shape<T, true>(team, D, [&](auto t, auto it, auto whole) {
             constexpr int TEAM = decltype(t)::value, ITER = decltype(it)::value;
