@@ -166,7 +166,7 @@ def selective_grad(dy, A, dt, Bm, Cm, u, h0=None, dt_bias=None, z=None, lengths=
             if z is not None:
                 p = sigmoid(z[b, t])
                 o = (Cw[b, t] * xs[t + 1]).sum(1) + h0 * u[b, t]
-                out["dz"][b, t] = d * o * _mag(p * (1 + z[b, t] * (1 - p)), magnitude)
+                out["dz"][b, t] = d * o * p * (1 + _mag(z[b, t], magnitude) * (1 - p))
                 d = d * _mag(z[b, t] * p, magnitude)
             g = g + Cw[b, t] * d[:, None]
             step = (delta[b, t] * u[b, t])[:, None]
