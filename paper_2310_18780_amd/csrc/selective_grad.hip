@@ -90,9 +90,10 @@ struct Chunk {
 };
 
 // Every load of a chunk starts before the first is used (rows past the last are its
-// copies, and become zeros in LDS: there the state stays).
+// copies, and become zeros in LDS: there the state stays).  Returns whether this thread's
+// steps, inputs and d are all finite (false, too, where their sum overflows).
 template <typename T, int NS, int S, bool GATE>
-__device__ __forceinline__ void load_chunk(const Selective& s, const SelectiveGrads& g,
+__device__ __forceinline__ bool load_chunk(const Selective& s, const SelectiveGrads& g,
                                            const Place& p, Chunk<S, NS>& m)
 {
     constexpr int kChunk = chunk_steps(NS), R = kChunk / S;
@@ -125,6 +126,7 @@ __device__ __forceinline__ void load_chunk(const Selective& s, const SelectiveGr
         rB[i] = pB[j * s.ld_b + n];
         rC[i] = pC[j * s.ld_c + n];
     }
+    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int j = p.wave + i * S;
@@ -137,6 +139,7 @@ __device__ __forceinline__ void load_chunk(const Selective& s, const SelectiveGr
         if (j >= left) delta = du = d = 0.f;
         // (lanes past the group add nothing to the sums over channels)
         if (!p.own) du = d = 0.f;
+        sum += fabsf(delta) + (fabsf(du) + fabsf(d));
         m.delta[j][p.lane] = delta;
         m.du[j][p.lane] = du;
         m.d[j][p.lane] = d;
@@ -151,6 +154,7 @@ __device__ __forceinline__ void load_chunk(const Selective& s, const SelectiveGr
         }
     }
     __syncthreads();
+    return sum < INFINITY;
 }
 
 template <typename T, int NS, int S, bool GATE>
@@ -297,14 +301,26 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
     __shared__ float po[GATE ? S : 1][kBlockSteps][kWave], pp[S][kBlockSteps][kWave], pq[S][kBlockSteps][kWave];
     const Place p = place_of<NS>(s, nchunks);
     constexpr int kBlocks = chunk_steps(NS) / kBlockSteps;
-    load_chunk<T, NS, S, GATE>(s, g, p, m);
+    const bool finite = load_chunk<T, NS, S, GATE>(s, g, p, m);
+    // Slots past N hold zeros and add zeros to the sums over states, unless a step or an
+    // input is not finite: zero times infinity is not zero.  The form that leaves those slots
+    // out is taken by the whole workgroup, since both hold barriers.
+    bool guarded = false;
+    if (s.N < NS * S) {
+        if (p.lane == 0) pp[p.wave][0][0] = 0.f;
+        if (!finite) pp[p.wave][0][0] = 1.f;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < S; ++k) guarded |= pp[k][0][0] != 0.f;
+        __syncthreads();
+    }
 
-    float A[NS], A2[NS], x[NS], G[NS], dA[NS];
+    float A2[NS], x[NS], G[NS], dA[NS];
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         // (slots past N load the last state and become zeros, so that no load waits alone)
         const int n = i < p.real ? p.n0 + i : s.N - 1;
-        A[i] = s.A[p.c * s.N + n];
+        A2[i] = s.A[p.c * s.N + n];
         const int64_t at = ((p.b * nchunks + p.k) * s.N + n) * s.D + p.c;
         x[i] = w.xs[at];
         G[i] = w.gs[at];
@@ -312,18 +328,15 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
     }
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-        A[i] = i < p.real ? A[i] : 0.f;
+        A2[i] = i < p.real ? A2[i] * kLog2e : 0.f;
         x[i] = i < p.real ? x[i] : 0.f;
         G[i] = i < p.real ? G[i] : 0.f;
-        A2[i] = A[i] * kLog2e;
     }
     const float bias = s.dt_bias ? s.dt_bias[p.c] : 0.f, h0 = s.h0 ? s.h0[p.c] : 0.f;
     float dh0 = 0.f, dbias = 0.f;
     const int64_t row0 = p.b * s.T + p.t0, last = p.t1 - 1 - p.t0;
-    // FULL: all NS slots hold states.  (Else the sums leave out the others, since zero
-    // times an infinite input is not zero.)
-    auto walk = [&](auto full) {
-    constexpr bool FULL = decltype(full)::value;
+    auto walk = [&](auto plain) {
+    constexpr bool PLAIN = decltype(plain)::value;
     // the state at the start of every block
     float start[kBlocks][NS];
 #pragma unroll
@@ -374,7 +387,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
                 a[j][i] = exp2_fast(delta * A2[i]);
                 before[j][i] = x[i];
                 x[i] = fmaf(a[j][i], x[i], du * m.B[j0 + j][p.n0 + i]);
-                if (FULL || i < p.real) o = fmaf(m.C[j0 + j][p.n0 + i], x[i], o);
+                if (PLAIN || i < p.real) o = fmaf(m.C[j0 + j][p.n0 + i], x[i], o);
             }
             if constexpr (GATE) po[p.wave][j][p.lane] = o;
         }
@@ -392,9 +405,9 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
                 v[i] = G[i] * du;
                 v[NS + i] = d * after;
                 const float ag = a[j][i] * G[i], h = ag * before[j][i];
-                if (FULL || i < p.real) {
+                if (PLAIN || i < p.real) {
                     pv = fmaf(G[i], m.B[j0 + j][p.n0 + i], pv);
-                    qv = fmaf(A[i], h, qv);
+                    qv = fmaf(A2[i], h, qv);
                 }
                 dA[i] = fmaf(delta, h, dA[i]);
                 G[i] = ag;
@@ -452,6 +465,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
                 pv += pp[k][j][p.lane];
                 qv += pq[k][j][p.lane];
             }
+            qv *= kLn2;  // (A is held times log2 e alone)
             const float u = io_load(&ru[i]), d = m.d[j0 + j][p.lane];
             const float ddt = fmaf(u, pv, qv) * sigmoid(io_load(&rd[i]) + bias);
             io_store(&ddt_at, ddt);
@@ -469,7 +483,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
         __syncthreads();
     }
     };
-    if (p.real == NS)
+    if (!__builtin_amdgcn_readfirstlane(guarded))
         walk(std::true_type());
     else
         walk(std::false_type());
