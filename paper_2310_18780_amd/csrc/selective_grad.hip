@@ -50,6 +50,7 @@ struct GradWork {
 struct Place {
     int64_t tile, k, b, grp, c0, c, t0, t1, te;
     int lane, wave, n0, real;
+    int left;     // of the chunk's steps, those that are tokens of the row
     uint32_t lc;  // the lane's channel in the tile (past the group: the last)
     bool own;
 };
@@ -78,6 +79,7 @@ __device__ __forceinline__ Place place_of(const Selective& s, int64_t nchunks)
     p.t0 = p.k * chunk;
     p.t1 = p.t0 + chunk < s.T ? p.t0 + chunk : s.T;
     p.te = p.t1 < len ? p.t1 : len;
+    p.left = p.te > p.t0 ? int(p.te - p.t0) : 0;
     return p;
 }
 
@@ -89,8 +91,8 @@ struct Chunk {
     float B[kChunk][S * NS], C[kChunk][S * NS];
 };
 
-// Every load of a chunk starts before the first is used (rows past the last are its
-// copies, and become zeros in LDS: there the state stays).  Returns whether this thread's
+// Every load of a chunk starts before the first is used (rows past the last token are its
+// copies, and become zeros in LDS).  The chunk has a token.  Returns whether this thread's
 // steps, inputs and d are all finite (false, too, where their sum overflows).
 template <typename T, int NS, int S, bool GATE>
 __device__ __forceinline__ bool load_chunk(const Selective& s, const SelectiveGrads& g,
@@ -98,9 +100,8 @@ __device__ __forceinline__ bool load_chunk(const Selective& s, const SelectiveGr
 {
     constexpr int kChunk = chunk_steps(NS), R = kChunk / S;
     constexpr int PER = (kChunk * NS + kWave - 1) / kWave;  // elements of B (of C) per thread
-    const int left = int(p.te - p.t0 < 0 ? 0 : p.te - p.t0);
-    const int64_t row0 = p.b * s.T + (left > 0 ? p.t0 : 0);
-    const int last = left > 0 ? left - 1 : 0;
+    const int left = p.left, last = left - 1;
+    const int64_t row0 = p.b * s.T + p.t0;
     const uint32_t off = p.lc * sizeof(T);
     const T* pu = static_cast<const T*>(s.u) + row0 * s.ld_u + p.c0;
     const T* pdt = static_cast<const T*>(s.dt) + row0 * s.ld_dt + p.c0;
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(kWave* S) void grad_ends_kernel(Selective s, Select
 {
     __shared__ Chunk<S, NS> m;
     const Place p = place_of<NS>(s, nchunks);
-    load_chunk<T, NS, S, GATE>(s, g, p, m);
+    if (p.left > 0) load_chunk<T, NS, S, GATE>(s, g, p, m);
     float A2[NS], x[NS], dec[NS], r[NS], total = 0.f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
@@ -173,18 +174,27 @@ __global__ __launch_bounds__(kWave* S) void grad_ends_kernel(Selective s, Select
     }
 #pragma unroll
     for (int i = 0; i < NS; ++i) A2[i] = i < p.real ? A2[i] * kLog2e : 0.f;
+    // (steps past the row's tokens are not walked: zero times an infinite state or pole is
+    // not zero)
+    auto walk = [&](auto steps) {
 #pragma unroll 4
-    for (int j = 0; j < chunk_steps(NS); ++j) {
-        const float delta = m.delta[j][p.lane], du = m.du[j][p.lane], d = m.d[j][p.lane];
-        total += delta;
+        for (int j = 0; j < steps; ++j) {
+            const float delta = m.delta[j][p.lane], du = m.du[j][p.lane], d = m.d[j][p.lane];
+            total += delta;
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const float a = exp2_fast(delta * A2[i]);
-            x[i] = fmaf(a, x[i], du * m.B[j][p.n0 + i]);
-            dec[i] *= a;  // decay from the chunk's start through step j
-            r[i] = fmaf(dec[i] * m.C[j][p.n0 + i], d, r[i]);
+            for (int i = 0; i < NS; ++i) {
+                const float a = exp2_fast(delta * A2[i]);
+                x[i] = fmaf(a, x[i], du * m.B[j][p.n0 + i]);
+                dec[i] *= a;  // decay from the chunk's start through step j
+                r[i] = fmaf(dec[i] * m.C[j][p.n0 + i], d, r[i]);
+            }
         }
-    }
+    };
+    constexpr int kChunk = chunk_steps(NS);
+    if (p.left == kChunk)
+        walk(std::integral_constant<int, kChunk>());
+    else
+        walk(p.left);
     if (!p.own) return;
 #pragma unroll
     for (int i = 0; i < NS; ++i)
@@ -227,7 +237,8 @@ __global__ __launch_bounds__(256) void grad_carry_kernel(const float* __restrict
         for (int i = 0; i < U; ++i)
             if (k + i < nchunks) {
                 px[(k + i) * sx] = x;
-                x = fmaf(exp2_fast(A2 * sum[i]), x, end[i]);
+                // (a chunk without tokens leaves x alone, also where A is infinite)
+                x = fmaf(exp2_fast(sum[i] == 0.f ? 0.f : A2 * sum[i]), x, end[i]);
             }
     }
 }
@@ -301,10 +312,27 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
     __shared__ float po[GATE ? S : 1][kBlockSteps][kWave], pp[S][kBlockSteps][kWave], pq[S][kBlockSteps][kWave];
     const Place p = place_of<NS>(s, nchunks);
     constexpr int kBlocks = chunk_steps(NS) / kBlockSteps;
+    const uint32_t off = p.lc * sizeof(T);
+    // gradients past the row's tokens are zero (of B and C: grad_rows_kernel)
+    if (p.own)
+        for (int64_t t = (p.te > p.t0 ? p.te : p.t0) + p.wave; t < p.t1; t += S) {
+            const int64_t row = (p.b * s.T + t) * s.D + p.c0;
+            io_store(&at_byte(static_cast<T*>(g.ddt) + row, off), 0.f);
+            io_store(&at_byte(static_cast<T*>(g.du) + row, off), 0.f);
+            if constexpr (GATE) io_store(&at_byte(static_cast<T*>(g.dz) + row, off), 0.f);
+        }
+    float* part = w.part + (p.b * nchunks + p.k) * (s.D * s.N + 2 * s.D);
+    if (p.left == 0) {
+        if (!p.own) return;
+        for (int i = 0; i < p.real; ++i) part[p.c * s.N + p.n0 + i] = 0.f;
+        if (p.wave == 0) part[s.D * s.N + p.c] = part[s.D * s.N + s.D + p.c] = 0.f;
+        return;
+    }
     const bool finite = load_chunk<T, NS, S, GATE>(s, g, p, m);
-    // Slots past N hold zeros and add zeros to the sums over states, unless a step or an
-    // input is not finite: zero times infinity is not zero.  The form that leaves those slots
-    // out is taken by the whole workgroup, since both hold barriers.
+    // Slots past N and steps past the row's tokens hold zeros and add zeros to the sums, unless
+    // a step, an input or the state that the tokens leave is not finite: zero times infinity is
+    // not zero.  The guarded form of a block leaves both out.  A whole workgroup takes the same
+    // form, since both hold barriers.
     bool guarded = false;
     if (s.N < NS * S) {
         if (p.lane == 0) pp[p.wave][0][0] = 0.f;
@@ -334,9 +362,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
     }
     const float bias = s.dt_bias ? s.dt_bias[p.c] : 0.f, h0 = s.h0 ? s.h0[p.c] : 0.f;
     float dh0 = 0.f, dbias = 0.f;
-    const int64_t row0 = p.b * s.T + p.t0, last = p.t1 - 1 - p.t0;
-    auto walk = [&](auto plain) {
-    constexpr bool PLAIN = decltype(plain)::value;
+    const int64_t row0 = p.b * s.T + p.t0, last = p.left - 1;
     // the state at the start of every block
     float start[kBlocks][NS];
 #pragma unroll
@@ -354,145 +380,149 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
         }
     }
 
+    // Blocks from - 1 down to `to`.
+    auto walk = [&](auto plain, int from, int to) {
+        constexpr bool PLAIN = decltype(plain)::value;
 #pragma unroll 1
-    for (int q = kBlocks - 1; q >= 0; --q) {
-        // registers are indexed by constants: the block's start is picked by comparison
+        for (int q = from - 1; q >= to; --q) {
+            // registers are indexed by constants: the block's start is picked by comparison
 #pragma unroll
-        for (int z = 0; z < kBlocks; ++z)
-            if (z == q)
+            for (int z = 0; z < kBlocks; ++z)
+                if (z == q)
 #pragma unroll
-                for (int i = 0; i < NS; ++i) x[i] = start[z][i];
-        float before[kBlockSteps][NS], a[kBlockSteps][NS];
-        const int j0 = q * kBlockSteps;
-        // what this wavefront's rows of the block need beside the sums, loaded ahead
-        constexpr int kRows = (kBlockSteps + S - 1) / S;
-        T ru[kRows], rd[kRows], rz[kRows], rg[kRows];
-        const uint32_t off = p.lc * sizeof(T);
+                    for (int i = 0; i < NS; ++i) x[i] = start[z][i];
+            float before[kBlockSteps][NS], a[kBlockSteps][NS];
+            const int j0 = q * kBlockSteps;
+            // what this wavefront's rows of the block need beside the sums, loaded ahead
+            constexpr int kRows = (kBlockSteps + S - 1) / S;
+            T ru[kRows], rd[kRows], rz[kRows], rg[kRows];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int64_t j = j0 + p.wave + i * S < last ? j0 + p.wave + i * S : last;
-            ru[i] = at_byte(static_cast<const T*>(s.u) + (row0 + j) * s.ld_u + p.c0, off);
-            rd[i] = at_byte(static_cast<const T*>(s.dt) + (row0 + j) * s.ld_dt + p.c0, off);
-            if constexpr (GATE) {
-                rz[i] = at_byte(static_cast<const T*>(s.z) + (row0 + j) * s.ld_z + p.c0, off);
-                rg[i] = at_byte(static_cast<const T*>(g.dy) + (row0 + j) * s.D + p.c0, off);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kBlockSteps; ++j) {
-            const float delta = m.delta[j0 + j][p.lane], du = m.du[j0 + j][p.lane];
-            float o = 0.f;
-#pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                a[j][i] = exp2_fast(delta * A2[i]);
-                before[j][i] = x[i];
-                x[i] = fmaf(a[j][i], x[i], du * m.B[j0 + j][p.n0 + i]);
-                if (PLAIN || i < p.real) o = fmaf(m.C[j0 + j][p.n0 + i], x[i], o);
-            }
-            if constexpr (GATE) po[p.wave][j][p.lane] = o;
-        }
-        float folded[kBlockSteps];
-        constexpr int kTop = 64 / (2 * NS);  // lane bits below kTop are left after a step's folds
-#pragma unroll
-        for (int j = kBlockSteps - 1; j >= 0; --j) {
-            const float delta = m.delta[j0 + j][p.lane], du = m.du[j0 + j][p.lane],
-                        d = m.d[j0 + j][p.lane];
-            float pv = 0.f, qv = 0.f, v[2 * NS];
-#pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                G[i] = fmaf(m.C[j0 + j][p.n0 + i], d, G[i]);
-                const float after = j < kBlockSteps - 1 ? before[j < kBlockSteps - 1 ? j + 1 : 0][i] : x[i];
-                v[i] = G[i] * du;
-                v[NS + i] = d * after;
-                const float ag = a[j][i] * G[i], h = ag * before[j][i];
-                if (PLAIN || i < p.real) {
-                    pv = fmaf(G[i], m.B[j0 + j][p.n0 + i], pv);
-                    qv = fmaf(A2[i], h, qv);
+            for (int i = 0; i < kRows; ++i) {
+                const int64_t j = j0 + p.wave + i * S < last ? j0 + p.wave + i * S : last;
+                ru[i] = at_byte(static_cast<const T*>(s.u) + (row0 + j) * s.ld_u + p.c0, off);
+                rd[i] = at_byte(static_cast<const T*>(s.dt) + (row0 + j) * s.ld_dt + p.c0, off);
+                if constexpr (GATE) {
+                    rz[i] = at_byte(static_cast<const T*>(s.z) + (row0 + j) * s.ld_z + p.c0, off);
+                    rg[i] = at_byte(static_cast<const T*>(g.dy) + (row0 + j) * s.D + p.c0, off);
                 }
-                dA[i] = fmaf(delta, h, dA[i]);
-                G[i] = ag;
             }
-            pp[p.wave][j][p.lane] = pv;
-            pq[p.wave][j][p.lane] = qv;
-            folded[j] = fold_all<2 * NS, 32>(v, p.lane);
-        }
-        // fold the block's steps into the lane bits that are left
-        constexpr int kHalf = kTop / 2 ? kTop / 2 : 1;
-        if constexpr (kTop == kBlockSteps) {  // every lane ends with one sum
-            const float r = fold_all<kBlockSteps, kHalf>(folded, p.lane);
-            // lane bits from the top: log2(2 NS) of the value, 3 of the step, each lowest first
-            int v = 0, j = 0;
-#pragma unroll
-            for (int bit = 0; (1 << bit) < 2 * NS; ++bit) v |= ((p.lane >> (5 - bit)) & 1) << bit;
-#pragma unroll
-            for (int bit = 0; (1 << bit) < kBlockSteps; ++bit)
-                j |= ((p.lane >> (5 - (6 - __builtin_ctz(kBlockSteps)) - bit)) & 1) << bit;
-            const int i = v % NS, which = v / NS;
-            if (i < p.real && p.t0 + j0 + j < p.t1)
-                w.rows[((p.tile * s.B * s.T) + row0 + j0 + j) * 2 * s.N + which * s.N + p.n0 + i] = r;
-        } else {
 #pragma unroll
             for (int j = 0; j < kBlockSteps; ++j) {
-                const float r = sum_below<kTop / 2>(folded[j], p.lane);
-                int v = 0;
+                const float delta = m.delta[j0 + j][p.lane], du = m.du[j0 + j][p.lane];
+                float o = 0.f;
+                if (!PLAIN && j0 + j > last) {
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) a[j][i] = 1.f, before[j][i] = x[i];
+                    continue;
+                }
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                    a[j][i] = exp2_fast(delta * A2[i]);
+                    before[j][i] = x[i];
+                    x[i] = fmaf(a[j][i], x[i], du * m.B[j0 + j][p.n0 + i]);
+                    if (PLAIN || i < p.real) o = fmaf(m.C[j0 + j][p.n0 + i], x[i], o);
+                }
+                if constexpr (GATE) po[p.wave][j][p.lane] = o;
+            }
+            float folded[kBlockSteps];
+            constexpr int kTop = 64 / (2 * NS);  // lane bits below kTop are left after a step's folds
+#pragma unroll
+            for (int j = kBlockSteps - 1; j >= 0; --j) {
+                if (!PLAIN && j0 + j > last) {
+                    folded[j] = 0.f;
+                    continue;
+                }
+                const float delta = m.delta[j0 + j][p.lane], du = m.du[j0 + j][p.lane],
+                            d = m.d[j0 + j][p.lane];
+                float pv = 0.f, qv = 0.f, v[2 * NS];
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                    G[i] = fmaf(m.C[j0 + j][p.n0 + i], d, G[i]);
+                    const float after = j < kBlockSteps - 1 ? before[j < kBlockSteps - 1 ? j + 1 : 0][i] : x[i];
+                    v[i] = G[i] * du;
+                    v[NS + i] = d * after;
+                    const float ag = a[j][i] * G[i], h = ag * before[j][i];
+                    if (PLAIN || i < p.real) {
+                        pv = fmaf(G[i], m.B[j0 + j][p.n0 + i], pv);
+                        qv = fmaf(A2[i], h, qv);
+                    }
+                    dA[i] = fmaf(delta, h, dA[i]);
+                    G[i] = ag;
+                }
+                pp[p.wave][j][p.lane] = pv;
+                pq[p.wave][j][p.lane] = qv;
+                folded[j] = fold_all<2 * NS, 32>(v, p.lane);
+            }
+            // fold the block's steps into the lane bits that are left
+            constexpr int kHalf = kTop / 2 ? kTop / 2 : 1;
+            if constexpr (kTop == kBlockSteps) {  // every lane ends with one sum
+                const float r = fold_all<kBlockSteps, kHalf>(folded, p.lane);
+                // lane bits from the top: log2(2 NS) of the value, 3 of the step, each lowest first
+                int v = 0, j = 0;
 #pragma unroll
                 for (int bit = 0; (1 << bit) < 2 * NS; ++bit) v |= ((p.lane >> (5 - bit)) & 1) << bit;
+#pragma unroll
+                for (int bit = 0; (1 << bit) < kBlockSteps; ++bit)
+                    j |= ((p.lane >> (5 - (6 - __builtin_ctz(kBlockSteps)) - bit)) & 1) << bit;
                 const int i = v % NS, which = v / NS;
-                if (p.lane % kTop == 0 && i < p.real && p.t0 + j0 + j < p.t1)
+                if (i < p.real && j0 + j <= last)
                     w.rows[((p.tile * s.B * s.T) + row0 + j0 + j) * 2 * s.N + which * s.N + p.n0 + i] = r;
+            } else {
+#pragma unroll
+                for (int j = 0; j < kBlockSteps; ++j) {
+                    const float r = sum_below<kTop / 2>(folded[j], p.lane);
+                    int v = 0;
+#pragma unroll
+                    for (int bit = 0; (1 << bit) < 2 * NS; ++bit) v |= ((p.lane >> (5 - bit)) & 1) << bit;
+                    const int i = v % NS, which = v / NS;
+                    if (p.lane % kTop == 0 && i < p.real && j0 + j <= last)
+                        w.rows[((p.tile * s.B * s.T) + row0 + j0 + j) * 2 * s.N + which * s.N + p.n0 + i] = r;
+                }
             }
+            __syncthreads();
+            // the channels' gradients of the block's steps, shared out among the wavefronts
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int j = p.wave + i * S;
+                if (j >= kBlockSteps || j0 + j > last || !p.own) continue;
+                const int64_t row = (row0 + j0 + j) * s.D + p.c0;
+                T& ddt_at = at_byte(static_cast<T*>(g.ddt) + row, off);
+                T& du_at = at_byte(static_cast<T*>(g.du) + row, off);
+                T& dz_at = GATE ? at_byte(static_cast<T*>(g.dz) + row, off) : du_at;
+                float pv = 0.f, qv = 0.f;
+#pragma unroll
+                for (int k = 0; k < S; ++k) {
+                    pv += pp[k][j][p.lane];
+                    qv += pq[k][j][p.lane];
+                }
+                qv *= kLn2;  // (A is held times log2 e alone)
+                const float u = io_load(&ru[i]), d = m.d[j0 + j][p.lane];
+                const float ddt = fmaf(u, pv, qv) * sigmoid(io_load(&rd[i]) + bias);
+                io_store(&ddt_at, ddt);
+                io_store(&du_at, fmaf(m.delta[j0 + j][p.lane], pv, h0 * d));
+                dbias += ddt;
+                dh0 = fmaf(d, u, dh0);
+                if constexpr (GATE) {
+                    float o = h0 * u;
+#pragma unroll
+                    for (int k = 0; k < S; ++k) o += po[k][j][p.lane];
+                    const float z = io_load(&rz[i]), sg = sigmoid(z);
+                    io_store(&dz_at, io_load(&rg[i]) * o * (sg * fmaf(z, 1.f - sg, 1.f)));
+                }
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        // the channels' gradients of the block's steps, shared out among the wavefronts
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int j = p.wave + i * S;
-            const int64_t t = p.t0 + j0 + j;
-            if (j >= kBlockSteps || t >= p.t1 || !p.own) continue;
-            const int64_t row = (row0 + j0 + j) * s.D + p.c0;
-            T& ddt_at = at_byte(static_cast<T*>(g.ddt) + row, off);
-            T& du_at = at_byte(static_cast<T*>(g.du) + row, off);
-            T& dz_at = GATE ? at_byte(static_cast<T*>(g.dz) + row, off) : du_at;
-            if (t >= p.te) {
-                io_store(&du_at, 0.f);
-                io_store(&ddt_at, 0.f);
-                if constexpr (GATE) io_store(&dz_at, 0.f);
-                continue;
-            }
-            float pv = 0.f, qv = 0.f;
-#pragma unroll
-            for (int k = 0; k < S; ++k) {
-                pv += pp[k][j][p.lane];
-                qv += pq[k][j][p.lane];
-            }
-            qv *= kLn2;  // (A is held times log2 e alone)
-            const float u = io_load(&ru[i]), d = m.d[j0 + j][p.lane];
-            const float ddt = fmaf(u, pv, qv) * sigmoid(io_load(&rd[i]) + bias);
-            io_store(&ddt_at, ddt);
-            io_store(&du_at, fmaf(m.delta[j0 + j][p.lane], pv, h0 * d));
-            dbias += ddt;
-            dh0 = fmaf(d, u, dh0);
-            if constexpr (GATE) {
-                float o = h0 * u;
-#pragma unroll
-                for (int k = 0; k < S; ++k) o += po[k][j][p.lane];
-                const float z = io_load(&rz[i]), sg = sigmoid(z);
-                io_store(&dz_at, io_load(&rg[i]) * o * (sg * fmaf(z, 1.f - sg, 1.f)));
-            }
-        }
-        __syncthreads();
-    }
     };
-    if (!__builtin_amdgcn_readfirstlane(guarded))
-        walk(std::true_type());
-    else
-        walk(std::false_type());
+    // the guarded form for all blocks, or for the one that the tokens end in
+    const int blocks = (p.left + kBlockSteps - 1) / kBlockSteps;
+    const int guard = __builtin_amdgcn_readfirstlane(guarded) ? 0 : p.left / kBlockSteps;
+    walk(std::false_type(), blocks, guard);
+    walk(std::true_type(), guard, 0);
     // partial rows of the weights' gradients
     pp[p.wave][0][p.lane] = dh0;
     pp[p.wave][1][p.lane] = dbias;
     __syncthreads();
     if (!p.own) return;
-    float* part = w.part + (p.b * nchunks + p.k) * (s.D * s.N + 2 * s.D);
 #pragma unroll
     for (int i = 0; i < NS; ++i)
         if (i < p.real) part[p.c * s.N + p.n0 + i] = dA[i];
@@ -508,7 +538,8 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
     }
 }
 
-// dB and dC: the tiles of each group added.
+// dB and dC: the tiles of each group added; zero past the row's tokens (where no partial
+// rows are written).
 template <typename T>
 __global__ __launch_bounds__(256) void grad_rows_kernel(Selective s, const float* __restrict__ rows,
                                                         T* __restrict__ dB, T* __restrict__ dC)
@@ -521,8 +552,9 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(Selective s, const float
     const int v = int(id % N2);
     const int64_t per = group_tiles(s.D, s.G), stride = s.B * s.T * N2;
     const float* p = rows + grp * per * stride + row * N2 + v;
+    const bool token = !s.lengths || row % s.T < tokens_of(s.lengths, row / s.T, s.T);
     float acc = 0.f;
-    for (int64_t i = 0; i < per; ++i) acc += p[i * stride];
+    for (int64_t i = 0; i < (token ? per : 0); ++i) acc += p[i * stride];
     const int64_t at = (row * s.G + grp) * s.N;
     if (v < s.N)
         io_store(dB + at + v, acc);

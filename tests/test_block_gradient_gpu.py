@@ -98,3 +98,33 @@ def test_an_infinite_input_with_empty_slots(N, where):
         out[k][1, :, 5] = clean[k][1, :, 5]
         assert torch.equal(out[k], clean[k]), k
     assert torch.equal(out["dBm"][0], clean["dBm"][0]) and torch.equal(out["dCm"][0], clean["dCm"][0])
+
+
+@pytest.mark.parametrize("at", [37, 69])
+@pytest.mark.parametrize("N", [10, 16, 64])
+def test_an_infinite_input_leaves_padded_tokens_zero(N, at):
+    """Past a row's tokens every gradient is zero, whatever state the row ends in, and an
+    input of the last token does not reach dA, which holds states before a token only."""
+    lengths = [150, 70, 0]
+    c, dy = positive_case(3, 150, 70, N, seed=N)
+    c["u"][1, at, 5] = float("inf")
+    ref, mag = reference(c, dy, lengths)
+    assert np.isfinite(ref["dA"]).all() == (at == 69)
+    poison(dict(c, dy=dy), lengths, ["dt", "Bm", "Cm", "u", "z", "dy"])
+    out = gradient(c, dy, lengths)
+    compare(out, ref, mag, roundings(c))
+    for k in ("ddt", "du", "dz", "dBm", "dCm"):
+        assert not out[k][1, 70:].any() and not out[k][2].any(), k
+
+
+@pytest.mark.parametrize("lengths", [None, [200, 70]])
+@pytest.mark.parametrize("N", [10, 16])
+def test_poles_at_minus_infinity(N, lengths):
+    """A state without memory: e^(delta A) = 0.  Only ddt (A times that zero) and its sum
+    over tokens are NaN, in that channel."""
+    c, dy = positive_case(2, 200, 70, N, seed=N + 1)
+    c["A"][7, 3] = -float("inf")
+    ref, mag = reference(c, dy, lengths)
+    assert all(np.isfinite(ref[k]).all() for k in ("dA", "dBm", "dCm", "du", "dz", "dh0"))
+    out = gradient(c, dy, lengths)
+    compare(out, ref, mag, roundings(c))
