@@ -49,7 +49,7 @@ struct GradWork {
 // What a lane needs to know of its place.
 struct Place {
     int64_t tile, k, b, grp, c0, c, t0, t1, te;
-    int lane, wave, n0, real;
+    int lane, wave, n0, real, width;  // width: the tile's channels
     int left;     // of the chunk's steps, those that are tokens of the row
     uint32_t lc;  // the lane's channel in the tile (past the group: the last)
     bool own;
@@ -68,9 +68,9 @@ __device__ __forceinline__ Place place_of(const Selective& s, int64_t nchunks)
     p.b = rest / nchunks;
     p.grp = p.tile / per;
     p.c0 = p.grp * Dg + (p.tile % per) * kWave;
-    const int width = int((p.grp + 1) * Dg - p.c0 < kWave ? (p.grp + 1) * Dg - p.c0 : kWave);
-    p.own = p.lane < width;
-    p.lc = p.own ? p.lane : width - 1;
+    p.width = int((p.grp + 1) * Dg - p.c0 < kWave ? (p.grp + 1) * Dg - p.c0 : kWave);
+    p.own = p.lane < p.width;
+    p.lc = p.own ? p.lane : p.width - 1;
     p.c = p.c0 + p.lc;
     p.n0 = p.wave * NS;
     p.real = s.N - p.n0 < NS ? s.N - p.n0 : NS;
@@ -93,7 +93,7 @@ struct Chunk {
 
 // Every load of a chunk starts before the first is used (rows past the last token are its
 // copies, and become zeros in LDS).  The chunk has a token.  Returns whether this thread's
-// steps, inputs and d are all finite (false, too, where their sum overflows).
+// steps, inputs, d, B and C are all finite (false, too, where their sum overflows).
 template <typename T, int NS, int S, bool GATE>
 __device__ __forceinline__ bool load_chunk(const Selective& s, const SelectiveGrads& g,
                                            const Place& p, Chunk<S, NS>& m)
@@ -150,8 +150,10 @@ __device__ __forceinline__ bool load_chunk(const Selective& s, const SelectiveGr
         const int e = threadIdx.x + i * kWave * S, j = e / (S * NS), n = e % (S * NS);
         if (e < kChunk * S * NS) {
             const bool in = j < left && n < s.N;
-            m.B[j][n] = in ? io_load(&rB[i]) : 0.f;
-            m.C[j][n] = in ? io_load(&rC[i]) : 0.f;
+            const float bv = in ? io_load(&rB[i]) : 0.f, cv = in ? io_load(&rC[i]) : 0.f;
+            m.B[j][n] = bv;
+            m.C[j][n] = cv;
+            sum += fabsf(bv) + fabsf(cv);
         }
     }
     __syncthreads();
@@ -329,12 +331,12 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
         return;
     }
     const bool finite = load_chunk<T, NS, S, GATE>(s, g, p, m);
-    // Slots past N and steps past the row's tokens hold zeros and add zeros to the sums, unless
-    // a step, an input or the state that the tokens leave is not finite: zero times infinity is
-    // not zero.  The guarded form of a block leaves both out.  A whole workgroup takes the same
-    // form, since both hold barriers.
+    // Slots past N, steps past the row's tokens and lanes past the group hold zeros and add zeros
+    // to the sums, unless an input, or the state that the tokens leave, is not finite: zero times
+    // infinity is not zero.  The guarded form of a block leaves them out.  A whole workgroup takes
+    // the same form, since both hold barriers.
     bool guarded = false;
-    if (s.N < NS * S) {
+    if (s.N < NS * S || p.width < kWave) {
         if (p.lane == 0) pp[p.wave][0][0] = 0.f;
         if (!finite) pp[p.wave][0][0] = 1.f;
         __syncthreads();
@@ -357,8 +359,8 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         A2[i] = i < p.real ? A2[i] * kLog2e : 0.f;
-        x[i] = i < p.real ? x[i] : 0.f;
-        G[i] = i < p.real ? G[i] : 0.f;
+        x[i] = i < p.real && p.own ? x[i] : 0.f;
+        G[i] = i < p.real && p.own ? G[i] : 0.f;
     }
     const float bias = s.dt_bias ? s.dt_bias[p.c] : 0.f, h0 = s.h0 ? s.h0[p.c] : 0.f;
     float dh0 = 0.f, dbias = 0.f;
@@ -439,8 +441,8 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
                 for (int i = 0; i < NS; ++i) {
                     G[i] = fmaf(m.C[j0 + j][p.n0 + i], d, G[i]);
                     const float after = j < kBlockSteps - 1 ? before[j < kBlockSteps - 1 ? j + 1 : 0][i] : x[i];
-                    v[i] = G[i] * du;
-                    v[NS + i] = d * after;
+                    v[i] = PLAIN || p.own ? G[i] * du : 0.f;
+                    v[NS + i] = PLAIN || p.own ? d * after : 0.f;
                     const float ag = a[j][i] * G[i], h = ag * before[j][i];
                     if (PLAIN || i < p.real) {
                         pv = fmaf(G[i], m.B[j0 + j][p.n0 + i], pv);

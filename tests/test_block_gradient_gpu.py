@@ -128,3 +128,16 @@ def test_poles_at_minus_infinity(N, lengths):
     assert all(np.isfinite(ref[k]).all() for k in ("dA", "dBm", "dCm", "du", "dz", "dh0"))
     out = gradient(c, dy, lengths)
     compare(out, ref, mag, roundings(c))
+
+
+@pytest.mark.parametrize("where", ["u", "dy", "Bm", "Cm"])
+@pytest.mark.parametrize("D,G", [(70, 1), (6, 2), (64, 1)])
+def test_an_infinite_input_in_a_narrow_tile(D, G, where):
+    """Lanes past a group's channels repeat its last channel and add nothing to dBm and dCm,
+    also where that channel's state or gradient, or a row of B or C, is infinite."""
+    c, dy = positive_case(2, 128, D, 16, seed=D, G=G)
+    at = (1, 20, G - 1, 3) if where in ("Bm", "Cm") else (1, 20, D - 1)
+    (dy if where == "dy" else c[where])[at] = float("inf")
+    ref, mag = reference(c, dy)
+    assert not np.isnan(ref["dBm"]).any() and not np.isnan(ref["dCm"]).any()
+    compare(gradient(c, dy), ref, mag, roundings(c))
