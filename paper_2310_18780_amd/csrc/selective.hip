@@ -140,7 +140,8 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
             for (int j = 0; j < U; ++j)
                 if (j0 + j < k) {
 #pragma unroll
-                    for (int i = 0; i < NS; ++i) x[i] = fmaf(exp2_fast(A2[i] * d[j]), x[i], e[j][i]);
+                    for (int i = 0; i < NS; ++i)
+                        x[i] = fmaf(chunk_decay(A2[i], d[j]), x[i], e[j][i]);
                 }
         }
     }
@@ -149,10 +150,9 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
     // The next tile's values, in flight as they lie in memory: a conversion would wait
     // for them.  A lane's places in a tile are 32-bit byte offsets from the tile's first row,
     // the same for all tiles but the last, whose rows past the end are copies of the
-    // last (so that no load is under a branch) and become zeros in LDS.
+    // last (so that no load is under a branch) and are not walked.
     T du[R], dd[R], dz[R], dr[PER];
     uint32_t ou[R], od[R], oz[R], oe[PER];
-    int ej[PER];      // the row of this thread's elements of B and C
     bool of_c[PER];
     auto places = [&](int rows_left) {
         const int last = rows_left < kSteps ? rows_left - 1 : kSteps - 1;
@@ -166,10 +166,10 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             const int e = threadIdx.x + p * kWave * S, f = e % (S * W * NS);
-            ej[p] = e < E ? e / (S * W * NS) : 0;
+            const int j = e < E ? e / (S * W * NS) : 0;  // the row
             const int n = f / (W * NS) * NS + f % NS;
             of_c[p] = f / NS % W;
-            oe[p] = (uint32_t(ej[p] < last ? ej[p] : last) * uint32_t(of_c[p] ? s.ld_c : s.ld_b) +
+            oe[p] = (uint32_t(j < last ? j : last) * uint32_t(of_c[p] ? s.ld_c : s.ld_b) +
                      (n < N ? n : N - 1)) * sizeof(T);
         }
     };
@@ -195,14 +195,17 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
         nB += kSteps * s.ld_b;
         nC += kSteps * s.ld_c;
     };
-    // The steps of a tile for CNT states of this wavefront.  (Slots past N are not
-    // walked: zero times an infinite input is not zero.)
-    auto walk = [&](auto count) {
+    // The steps of a tile (TAIL: the first `left`) for CNT states of this wavefront.  (Slots
+    // past N and steps past the row's end are not walked as zeros: zero times an infinite
+    // input or pole is not zero.)
+    auto walk = [&](auto count, auto tail, int left) {
         constexpr int CNT = decltype(count)::value;
+        constexpr bool TAIL = decltype(tail)::value;
         // (fewer steps unrolled where their values from LDS would not fit the registers)
         constexpr int kUnroll = NS > 6 ? 2 : kSteps;
 #pragma unroll kUnroll
         for (int j = 0; j < kSteps; ++j) {
+            if (TAIL && j >= left) break;
             const float2 d = step[j][lane];
             float acc = 0.f;
 #pragma unroll
@@ -230,15 +233,13 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
             float2 d;
             d.x = softplus(io_load(&dd[r]) + bias);
             d.y = d.x * cu[r];
-            // a step past the row's end is 0: the state stays
-            if (TAIL && j >= left) d = make_float2(0.f, 0.f);
             step[j][lane] = d;
         }
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             const int e = threadIdx.x + p * kWave * S;
             if (E % (kWave * S) == 0 || e < E)
-                (&rows[0][0][0][0])[e] = !TAIL || ej[p] < left ? io_load(&dr[p]) : 0.f;
+                (&rows[0][0][0][0])[e] = io_load(&dr[p]);
         }
         __syncthreads();
         const int64_t after = te - t0 - kSteps;  // rows left for the next tile
@@ -248,9 +249,9 @@ __global__ __launch_bounds__(kWave* S) void scan_kernel(Selective s, int64_t chu
         }
         load();  // (after the last tile: that tile again)
         if (real == NS)
-            walk(std::integral_constant<int, NS>());
+            walk(std::integral_constant<int, NS>(), tail, left);
         else
-            with_count<NS - 1>(real, walk);
+            with_count<NS - 1>(real, [&](auto count) { walk(count, tail, left); });
         __syncthreads();
         if constexpr (OUT) {
             T* row = py + t0 * s.D;
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(256) void carry_kernel(const float* __restrict__ A,
         for (int i = 0; i < U; ++i)
             if (k + i < nchunks) {
                 px[(k + i) * N * D] = x;
-                if (k + i < nchunks - 1) x = fmaf(exp2_fast(A2 * a[i]), x, end[i]);
+                if (k + i < nchunks - 1) x = fmaf(chunk_decay(A2, a[i]), x, end[i]);
             }
     }
 }

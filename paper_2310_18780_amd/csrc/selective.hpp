@@ -69,4 +69,11 @@ __device__ __forceinline__ int64_t tokens_of(const int* lengths, int64_t b, int6
     return n < 0 ? 0 : n < T ? n : T;
 }
 
+// The decay over a chunk whose steps sum to `sum`, A2 = A log2 e.  A chunk without tokens
+// leaves the state alone, also where A is infinite.
+__device__ __forceinline__ float chunk_decay(float A2, float sum)
+{
+    return exp2_fast(sum == 0.f ? 0.f : A2 * sum);
+}
+
 }  // namespace lh

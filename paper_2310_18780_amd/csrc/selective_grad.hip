@@ -239,8 +239,7 @@ __global__ __launch_bounds__(256) void grad_carry_kernel(const float* __restrict
         for (int i = 0; i < U; ++i)
             if (k + i < nchunks) {
                 px[(k + i) * sx] = x;
-                // (a chunk without tokens leaves x alone, also where A is infinite)
-                x = fmaf(exp2_fast(sum[i] == 0.f ? 0.f : A2 * sum[i]), x, end[i]);
+                x = fmaf(chunk_decay(A2, sum[i]), x, end[i]);
             }
     }
 }
