@@ -136,7 +136,9 @@ lh_status check_conv_sizes(int64_t B, int64_t T, int64_t D, int64_t K)
     return check_threads(lh::short_conv_threads(B, T, D, K));
 }
 
-lh_status check_selective_sizes(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G, bool grad)
+enum class Form { kPrompt, kStep, kGradient };
+
+lh_status check_selective_sizes(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G, Form form)
 {
     lh_status s;
     if ((s = check_at_least("B", B, 1)) || (s = check_at_least("T", T, 0)) ||
@@ -151,16 +153,18 @@ lh_status check_selective_sizes(int64_t B, int64_t T, int64_t D, int64_t N, int6
     // (the gradient's partial sums take G N floats per tile and token)
     if ((s = check_product("B, T, D, N", B, T, D, N)) || (s = check_product("G", G, INT64_C(1) << 30)))
         return s;
-    return check_threads(lh::selective_threads(B, T, D, int(N), int(G), grad));
+    return check_threads(form == Form::kStep     ? lh::selective_step_threads(B, D, int(N))
+                         : form == Form::kPrompt ? lh::selective_threads(B, T, D, int(N), int(G))
+                                                 : lh::selective_grad_threads(B, T, D, int(N), int(G)));
 }
 
-// The struct's pointers and sizes; `step` for single tokens.
-lh_status check_selective(const lh_selective_inputs* in, bool step, bool grad)
+// The struct's pointers and sizes.
+lh_status check_selective(const lh_selective_inputs* in, Form form)
 {
     lh_status s;
     if (!in) return fail(LH_ERR_INVALID_ARG, "inputs must not be NULL");
-    if ((s = check_selective_sizes(in->B, in->T, in->D, in->N, in->G, grad))) return s;
-    if (step && (in->T != 1 || in->lengths))
+    if ((s = check_selective_sizes(in->B, in->T, in->D, in->N, in->G, form))) return s;
+    if (form == Form::kStep && (in->T != 1 || in->lengths))
         return fail(LH_ERR_INVALID_ARG, "a step needs T = 1 and no lengths");
     if ((s = check_dtype(in->io_dtype))) return s;
     if (!in->A) return fail(LH_ERR_INVALID_ARG, "A must not be NULL");
@@ -364,7 +368,7 @@ lh_status lh_short_conv_backward(const void* dy, const void* x, int64_t ld_x, co
 
 size_t lh_selective_workspace_bytes(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G)
 {
-    if (check_selective_sizes(B, T, D, N, G, false) != LH_OK) return (size_t)-1;
+    if (check_selective_sizes(B, T, D, N, G, Form::kPrompt) != LH_OK) return (size_t)-1;
     return lh::selective_plan(B, T, D, int(N), int(G)).ws_bytes;
 }
 
@@ -373,7 +377,7 @@ lh_status lh_selective_prefill(const lh_selective_inputs* in, int resume, float*
 {
     g_last_error[0] = '\0';
     lh_status s;
-    if ((s = check_selective(in, false, false))) return s;
+    if ((s = check_selective(in, Form::kPrompt))) return s;
     if (!state || (in->T > 0 && !y))
         return fail(LH_ERR_INVALID_ARG, "state and y must not be NULL");
     const size_t es = esize(in->io_dtype);
@@ -395,7 +399,7 @@ lh_status lh_selective_step(const lh_selective_inputs* in, float* state, void* y
 {
     g_last_error[0] = '\0';
     lh_status s;
-    if ((s = check_selective(in, true, false))) return s;
+    if ((s = check_selective(in, Form::kStep))) return s;
     if (!state || !y_t) return fail(LH_ERR_INVALID_ARG, "state and y_t must not be NULL");
     const size_t es = esize(in->io_dtype);
     Arg ins[9];
@@ -410,7 +414,7 @@ lh_status lh_selective_step(const lh_selective_inputs* in, float* state, void* y
 
 size_t lh_selective_backward_workspace_bytes(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G)
 {
-    if (check_selective_sizes(B, T, D, N, G, true) != LH_OK) return (size_t)-1;
+    if (check_selective_sizes(B, T, D, N, G, Form::kGradient) != LH_OK) return (size_t)-1;
     return lh::selective_grad_workspace_bytes(B, T, D, int(N), int(G));
 }
 
@@ -419,7 +423,7 @@ lh_status lh_selective_backward(const lh_selective_inputs* in, const lh_selectiv
 {
     g_last_error[0] = '\0';
     lh_status s;
-    if ((s = check_selective(in, false, true))) return s;
+    if ((s = check_selective(in, Form::kGradient))) return s;
     if (!g || !g->dA) return fail(LH_ERR_INVALID_ARG, "gradients and dA must not be NULL");
     if (in->T > 0 && (!g->dy || !g->ddt || !g->du || !g->dBm || !g->dCm))
         return fail(LH_ERR_INVALID_ARG, "dy, ddt, du, dBm and dCm must not be NULL when T > 0");

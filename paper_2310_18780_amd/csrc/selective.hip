@@ -431,12 +431,19 @@ hipError_t scan(const Selective& s, float* state, bool resume, T* y, void* works
     });
 }
 
+// States to a lane of a step, and lanes to a row (a power of two).
+int step_states(int N) { return N >= 4 ? 4 : 1; }
+int step_lanes(int N)
+{
+    int lpr = 1;
+    while (lpr * step_states(N) < N) lpr *= 2;
+    return lpr;
+}
+
 template <typename T>
 hipError_t scan_step(const Selective& s, float* state, T* y, hipStream_t stream)
 {
-    const int V = s.N >= 4 ? 4 : 1;
-    int lpr = 1;
-    while (lpr * V < s.N) lpr *= 2;
+    const int V = step_states(s.N), lpr = step_lanes(s.N);
     const dim3 grid(uint32_t((s.B * s.D * lpr + 255) / 256));
 #define LH_STEP(v, l) \
     if (V == v && lpr == l) \
@@ -487,6 +494,19 @@ SelectivePlan selective_plan(int64_t B, int64_t T, int64_t D, int N, int G)
         p.ws_bytes = p.off_sums + size_t(B) * p.nchunks * D * sizeof(float);
     }
     return p;
+}
+
+int64_t selective_threads(int64_t B, int64_t T, int64_t D, int N, int G)
+{
+    const SelectivePlan p = selective_plan(B, T, D, N, G);
+    const int64_t scan = B * p.nchunks * group_tiles(D, G) * G * kWave * p.waves;
+    const int64_t carry = p.nchunks > 1 ? B * D * N : 0;
+    return (scan > carry ? scan : carry) + 256;  // (the carry's last workgroup)
+}
+
+int64_t selective_step_threads(int64_t B, int64_t D, int N)
+{
+    return B * D * step_lanes(N) + 256;
 }
 
 hipError_t launch_selective(const Selective& s, float* state, bool resume, void* y,

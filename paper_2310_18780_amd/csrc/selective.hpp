@@ -36,8 +36,10 @@ struct SelectivePlan {
 };
 SelectivePlan selective_plan(int64_t B, int64_t T, int64_t D, int N, int G);
 
-// Threads of the largest launch.
-int64_t selective_threads(int64_t B, int64_t T, int64_t D, int N, int G, bool grad);
+// Threads of the largest launch of a prompt, a step and a gradient.
+int64_t selective_threads(int64_t B, int64_t T, int64_t D, int N, int G);
+int64_t selective_step_threads(int64_t B, int64_t D, int N);
+int64_t selective_grad_threads(int64_t B, int64_t T, int64_t D, int N, int G);
 
 hipError_t launch_selective(const Selective& s, float* state, bool resume, void* y,
                             void* workspace, hipStream_t stream);

@@ -654,18 +654,16 @@ size_t selective_grad_workspace_bytes(int64_t B, int64_t T, int64_t D, int N, in
     return grad_work(B, T, D, N, G, nullptr, nullptr);
 }
 
-int64_t selective_threads(int64_t B, int64_t T, int64_t D, int N, int G, bool grad)
+int64_t selective_grad_threads(int64_t B, int64_t T, int64_t D, int N, int G)
 {
-    const int64_t tiles = group_tiles(D, G) * G;
-    int64_t most = B * D * (2 * int64_t(N) + 64);  // carries and steps
+    int ns = 0, waves = 0;
+    split_grad(N, &ns, &waves);
+    int64_t most = 32 * D * (int64_t(N) + 2);  // column sums
     auto at_least = [&](int64_t n) { most = n > most ? n : most; };
-    at_least(B * selective_plan(B, T, D, N, G).nchunks * tiles * 1024);
-    if (grad) {
-        at_least(B * grad_chunks(T, N) * tiles * (N <= 16 ? 256 : N <= 64 ? 512 : 1024));
-        at_least(B * T * G * 2 * N);
-        at_least(32 * D * (N + 2));  // column sums
-    }
-    return most + 1024;
+    at_least(B * grad_chunks(T, N) * group_tiles(D, G) * G * kWave * waves);
+    at_least(2 * B * D * N);      // carry
+    at_least(B * T * G * 2 * N);  // rows of B and C
+    return most + 1024;           // (the last workgroup)
 }
 
 hipError_t launch_selective_grad(const Selective& s, const SelectiveGrads& g, void* workspace,

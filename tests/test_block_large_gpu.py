@@ -1,0 +1,42 @@
+"""The selective block's calls at sizes whose offsets pass 32 bits, against the oracle on the
+last rows.  Tolerances are those derived in ``test_block_gpu``."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import oracle.block as ob
+import paper_2310_18780_amd as lh
+from test_block_gpu import check, dev, gen, host, np64
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need a HIP device"
+    lh.lib()
+    yield
+
+
+def randn(seed, *shape, dtype=torch.bfloat16):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.empty(shape, dtype=dtype, device="cuda").normal_(generator=g)
+
+
+def test_a_step_of_many_sessions():
+    B, D, N = 32768, 2048, 16  # 4.3 GB of state
+    r = gen(40)
+    c = dict(A=dev(-abs(r.normal(size=(D, N))) - 0.1), h0=dev(r.normal(size=D)), dt_bias=dev(r.normal(size=D) - 2))
+    rows = dict(dt=randn(1, B, D), u=randn(2, B, D), z=randn(3, B, D), Bm=randn(4, B, 1, N), Cm=randn(5, B, 1, N))
+    state = randn(6, B, D, N, dtype=torch.float32)
+    last = slice(B - 2, B)
+    args = dict(host(c), **{k: np64(v[last])[:, None] for k, v in rows.items()}, state=np64(state[last]))
+    ref, xref = ob.selective(**args)
+    mag, xmag = ob.selective(**args, magnitude=True)
+    y = torch.full((B, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lh.selective_step(c["A"], rows["dt"], rows["Bm"], rows["Cm"], rows["u"], state, y, h0=c["h0"], dt_bias=c["dt_bias"],
+                      z=rows["z"])
+    check(y[last], ref[:, 0], mag[:, 0], 3 + N + 64, "bf16", "y")
+    check(state[last], xref, xmag, 3 + N + 64, name="state")
+    assert torch.isfinite(y).all()

@@ -1,0 +1,47 @@
+"""Sizes that the selective block's entry points take (no GPU needed: a call whose sizes
+pass is refused for a later reason, here an output over an input)."""
+from __future__ import annotations
+
+import ctypes
+
+import paper_2310_18780_amd as lh
+
+A = 1 << 44
+INVALID, OVERLAP = 1, 2
+BAD = ctypes.c_size_t(-1).value
+
+
+def inputs(B, T, D, N, G=1, gap=1 << 40, **kw):
+    s = lh._SelectiveInputs()
+    a = dict(A=A, dt=A + gap, u=A + 2 * gap, Bm=A + 3 * gap, Cm=A + 4 * gap, ld_dt=D, ld_u=D, ld_B=G * N, ld_C=G * N, B=B, T=T,
+             D=D, N=N, G=G, io_dtype=1)
+    a.update(kw)
+    for k, v in a.items():
+        setattr(s, k, v)
+    return s
+
+
+def step(*sizes, **kw):
+    return lh.lib().lh_selective_step(ctypes.byref(inputs(sizes[0], 1, *sizes[1:], **kw)), A + 5 * (1 << 40), A + (1 << 40), None)
+
+
+def prefill(*sizes, **kw):
+    return lh.lib().lh_selective_prefill(ctypes.byref(inputs(*sizes, **kw)), 0, A + 5 * (1 << 40), A + (1 << 40), None, 0, None)
+
+
+def test_many_sessions_take_a_step():
+    # 32768 sessions of 2048 channels with 16 states (4.3 GB of state): 2^28 threads
+    assert step(32768, 2048, 16) == OVERLAP
+    assert step(1 << 20, 2048, 4) == OVERLAP  # 2^31 threads
+    assert step(1 << 20, 4096, 4) == INVALID and b"threads" in lh.lib().lh_last_error()  # 2^32
+    assert step(1 << 17, 2048, 128) == INVALID  # 2^28 rows of 32 lanes
+
+
+def test_large_batches_take_a_prompt_and_a_gradient():
+    # 4 wavefronts to each of 2^20 tiles
+    assert prefill(32768, 1, 2048, 16) == OVERLAP
+    assert lh.selective_workspace_bytes(32768, 1, 2048, 16) == 0
+    assert prefill(1 << 19, 1, 2048, 16) == INVALID and b"threads" in lh.lib().lh_last_error()
+    assert 0 < lh.selective_backward_workspace_bytes(32768, 1, 2048, 16) < BAD
+    # the gradient's carry: two threads to each of 2^31 states
+    assert lh.lib().lh_selective_backward_workspace_bytes(1 << 16, 1, 2048, 16, 1) == BAD
