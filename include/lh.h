@@ -579,7 +579,8 @@ size_t lh_selective_workspace_bytes(int64_t B, int64_t T, int64_t D, int64_t N, 
  *   y         : out [B, T, D] (io_dtype)
  *   workspace : lh_selective_workspace_bytes bytes, 256-byte aligned (NULL allowed when
  *               that is 0)
- * One kernel launch, or three where the prompt is cut into chunks.
+ * Every ld must be less than 2^26 here (not in a step or in the gradient).
+ * One kernel launch, or two or three where the prompt is cut into chunks.
  */
 lh_status lh_selective_prefill(const lh_selective_inputs* in, int resume, float* state, void* y,
                                void* workspace, size_t workspace_bytes, void* stream);

@@ -175,7 +175,8 @@ lh_status check_selective(const lh_selective_inputs* in, Form form)
         (in->z && (s = check_ld("ld_z", in->ld_z, in->D, rows))) ||
         (s = check_ld("ld_B", in->ld_B, w, rows)) || (s = check_ld("ld_C", in->ld_C, w, rows)))
         return s;
-    // (the rows of a tile are addressed in 32 bits)
+    // (a prompt addresses the rows of a tile in 32 bits)
+    if (form != Form::kPrompt) return LH_OK;
     for (const int64_t ld : {in->ld_dt, in->ld_u, in->z ? in->ld_z : 0, in->ld_B, in->ld_C})
         if (ld >= (INT64_C(1) << 26))
             return fail(LH_ERR_INVALID_ARG, "rows must be less than 2^26 elements apart, got %lld",

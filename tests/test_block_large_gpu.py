@@ -40,3 +40,33 @@ def test_a_step_of_many_sessions():
     check(y[last], ref[:, 0], mag[:, 0], 3 + N + 64, "bf16", "y")
     check(state[last], xref, xmag, 3 + N + 64, name="state")
     assert torch.isfinite(y).all()
+
+
+def test_steps_and_a_gradient_on_rows_far_apart():
+    """Tokens taken as slices of a long buffer: rows 2^26 elements and more apart."""
+    B, D, N, far = 2, 70, 16, (1 << 26) + 5
+    r = gen(41)
+    wide = torch.full((B * far,), float("nan"), dtype=torch.bfloat16, device="cuda").view(B, far)
+    rows = {}
+    at = 3
+    for k, n in (("dt", D), ("u", D), ("Bm", N), ("Cm", N)):
+        wide[:, at:at + n] = dev(r.normal(size=(B, n)), "bf16")
+        rows[k] = wide[:, at:at + n]
+        at += n + 1
+    rows["Bm"], rows["Cm"] = rows["Bm"].unflatten(1, (1, N)), rows["Cm"].unflatten(1, (1, N))
+    c = dict(A=dev(-abs(r.normal(size=(D, N)))), h0=dev(r.normal(size=D)), dt_bias=dev(r.normal(size=D) - 2))
+    state = dev(r.normal(size=(B, D, N)))
+    args = dict(host(c), **{k: np64(v)[:, None] for k, v in rows.items()})
+    ref, xref = ob.selective(**args, state=np64(state))
+    mag, xmag = ob.selective(**args, state=np64(state), magnitude=True)
+    y = torch.empty((B, D), dtype=torch.bfloat16, device="cuda")
+    lh.selective_step(c["A"], rows["dt"], rows["Bm"], rows["Cm"], rows["u"], state, y, h0=c["h0"], dt_bias=c["dt_bias"])
+    check(y, ref[:, 0], mag[:, 0], 3 + N + 64, "bf16", "y")
+    check(state, xref, xmag, 3 + N + 64, name="state")
+    one = {k: v[:, None] for k, v in rows.items()}  # prompts of one token
+    dy = dev(r.normal(size=(B, 1, D)), "bf16")
+    out = {"d" + k: torch.full(v.shape, float("nan"), dtype=v.dtype, device="cuda") for k, v in {**c, **one}.items()}
+    lh.selective_backward(dy=dy, **c, **one, **out)
+    gref, gmag = ob.selective_grad(np64(dy), **args), ob.selective_grad(np64(dy), **args, magnitude=True)
+    for k, v in out.items():
+        check(v, gref[k], gmag[k], 8 * B + D + N + 128, "bf16" if v.dtype is torch.bfloat16 else "f32", k)

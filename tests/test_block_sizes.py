@@ -45,3 +45,17 @@ def test_large_batches_take_a_prompt_and_a_gradient():
     assert 0 < lh.selective_backward_workspace_bytes(32768, 1, 2048, 16) < BAD
     # the gradient's carry: two threads to each of 2^31 states
     assert lh.lib().lh_selective_backward_workspace_bytes(1 << 16, 1, 2048, 16, 1) == BAD
+
+
+def test_rows_far_apart():
+    # token t of [B, 65536, 2048]: its rows lie 2^27 elements apart
+    far = dict(ld_dt=1 << 27, ld_u=1 << 27, ld_B=1 << 27, ld_C=1 << 27)
+    assert step(2, 2048, 16, **far) == OVERLAP
+    assert prefill(2, 1, 2048, 16, **far) == INVALID and b"2^26" in lh.lib().lh_last_error()
+    g = lh._SelectiveGrads()
+    for i, k in enumerate(("dy", "ddt", "du", "dBm", "dCm", "dA")):
+        setattr(g, k, A + (6 + i) * (1 << 40))
+    g.du = A + (1 << 40)  # over dt
+    need = lh.selective_backward_workspace_bytes(2, 1, 2048, 16)
+    assert lh.lib().lh_selective_backward(ctypes.byref(inputs(2, 1, 2048, 16, **far)), ctypes.byref(g), A + (13 << 40), need,
+                                          None) == OVERLAP
