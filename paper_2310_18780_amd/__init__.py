@@ -617,30 +617,39 @@ def _conv_args(x, w, bias, lead):
     return ld, D, K, _io_dtype(x)
 
 
+def _conv_state(state, dtype, B, K, D):
+    """Pointer of the state ``[B, K - 1, D]``; None is no state, which one tap leaves."""
+    if state is None and K == 1:
+        return None
+    _need(state, "state", dtype, (B, K - 1, D))
+    return state.data_ptr()
+
+
 def short_conv_prefill(x, w, bias, state, y, silu: bool = True, lengths=None, resume: bool = False,
                        stream=None) -> None:
     """Short causal convolution of the prompt ``x [B, T, D]`` with the taps ``w [D, K]``
     (``lh_short_conv_prefill``); ``state [B, K - 1, D]`` receives the last inputs, and is
-    what the prompt continues from where ``resume``.  ``x`` may be a slice of rows."""
+    what the prompt continues from where ``resume`` (None is taken with one tap).  ``x`` may
+    be a slice of rows."""
     B, T = x.shape[:2]
     ld, D, K, io = _conv_args(x, w, bias, (B, T))
-    _need(state, "state", x.dtype, (B, K - 1, D))
+    state_ptr = _conv_state(state, x.dtype, B, K, D)
     _need(y, "y", x.dtype, (B, T, D))
     _need_lengths(lengths, B)
     _check(lib().lh_short_conv_prefill(x.data_ptr(), ld, w.data_ptr(), _ptr(bias), _ptr(lengths), B,
-                                       T, D, K, io, silu, resume, state.data_ptr(), y.data_ptr(),
+                                       T, D, K, io, silu, resume, state_ptr, y.data_ptr(),
                                        _handle(x, stream)))
 
 
 def short_conv_step(x_t, w, bias, state, y_t, silu: bool = True, stream=None) -> None:
-    """One token per row, ``x_t``, ``y_t`` ``[B, D]``, ``state`` in place
-    (``lh_short_conv_step``)."""
+    """One token per row, ``x_t``, ``y_t`` ``[B, D]``, ``state`` in place (None is taken with
+    one tap) (``lh_short_conv_step``)."""
     B = x_t.shape[0]
     ld, D, K, io = _conv_args(x_t, w, bias, (B,))
-    _need(state, "state", x_t.dtype, (B, K - 1, D))
+    state_ptr = _conv_state(state, x_t.dtype, B, K, D)
     _need(y_t, "y_t", x_t.dtype, (B, D))
     _check(lib().lh_short_conv_step(x_t.data_ptr(), ld, w.data_ptr(), _ptr(bias), B, D, K, io, silu,
-                                    state.data_ptr(), y_t.data_ptr(), _handle(x_t, stream)))
+                                    state_ptr, y_t.data_ptr(), _handle(x_t, stream)))
 
 
 def short_conv_backward_workspace_bytes(B: int, T: int, D: int, K: int) -> int:
