@@ -141,3 +141,19 @@ def test_an_infinite_input_in_a_narrow_tile(D, G, where):
     ref, mag = reference(c, dy)
     assert not np.isnan(ref["dBm"]).any() and not np.isnan(ref["dCm"]).any()
     compare(gradient(c, dy), ref, mag, roundings(c))
+
+
+# more chunks than the carry takes at a time (8), and than twice that: 18 of 64 steps, 33 and
+# 41 of 32, with states that last over many chunks
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("case", [(1, 1100, 10, 8, 1, None), (2, 1030, 6, 33, 3, [1030, 333]), (1, 1312, 70, 64, 1, None),
+                                  (2, 640, 65, 16, 5, [600, 640])], ids=str)
+def test_many_chunks_and_slow_poles(case, io):
+    B, T, D, N, G, lengths = case
+    c = scan_case(case, io, seed=17)
+    c["A"] = dev(-np.exp(gen(T).normal(size=(D, N)) - 5))
+    dy = dev(gen(T + 2).normal(size=(B, T, D)), io)
+    ref, mag = reference(c, dy, lengths)
+    if lengths is not None:
+        poison(dict(c, dy=dy), lengths, ["dt", "Bm", "Cm", "u", "z", "dy"])
+    compare(gradient(c, dy, lengths, io), ref, mag, roundings(c), io)
