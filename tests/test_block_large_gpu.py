@@ -2,6 +2,7 @@
 last rows.  Tolerances are those derived in ``test_block_gpu``."""
 from __future__ import annotations
 
+import numpy as np
 import pytest
 import torch
 
@@ -70,3 +71,38 @@ def test_steps_and_a_gradient_on_rows_far_apart():
     gref, gmag = ob.selective_grad(np64(dy), **args), ob.selective_grad(np64(dy), **args, magnitude=True)
     for k, v in out.items():
         check(v, gref[k], gmag[k], 8 * B + D + N + 128, "bf16" if v.dtype is torch.bfloat16 else "f32", k)
+
+
+def test_gradients_past_32_bits():
+    """Tensors of more than 2^31 elements: the last tokens' gradients against the oracle on
+    those tokens and enough before them."""
+    T, D, N, tail, keep = (1 << 21) + 70, 1056, 2, 160, 40
+    dy, x = randn(1, 1, T, D), randn(2, 1, T, D)
+    last, own = slice(T - tail, T), slice(tail - keep, tail)
+    # layer norm: rows are independent
+    w, mean, rstd = dev(gen(1).normal(size=D)), torch.zeros((1, T), device="cuda"), torch.ones((1, T), device="cuda")
+    dx, dw = torch.empty_like(x), torch.empty(D, device="cuda")
+    lh.layer_norm_backward(dy, x, w, mean, rstd, dx, dw)
+    args = (np64(dy[0, last]), np64(x[0, last]), np64(w), np64(mean[0, last]), np64(rstd[0, last]))
+    check(dx[0, last], ob.layer_norm_grad(*args)[0], ob.layer_norm_grad(*args, magnitude=True)[0], 192, "bf16", "dx")
+    # convolution: a token's gradient needs K - 1 tokens on both sides
+    K = 4
+    taps, bias, dtaps = dev(gen(2).normal(size=(D, K))), dev(gen(3).normal(size=D)), torch.empty((D, K), device="cuda")
+    lh.short_conv_backward(dy, x, taps, bias, dx, dtaps)
+    args = dict(dy=np64(dy[:, last]), x=np64(x[:, last]), w=np64(taps), bias=np64(bias), silu=True)
+    ref, mag = ob.short_conv_grad(**args)[0], ob.short_conv_grad(**args, magnitude=True)[0]
+    check(dx[:, last][:, own], ref[:, own], mag[:, own], 3 * K + 24, "bf16", "dx")
+    # scan: steps of softplus(4 + N(0, 1)) > 0.1 and poles below -8 leave less than e^-90 of a
+    # state after 120 tokens
+    r = gen(4)
+    A, dt_bias, h0 = dev(-8 - r.random(size=(D, N))), dev(np.full(D, 4.0)), dev(r.normal(size=D))
+    rows = randn(3, 1, T, 1, 2 * N)
+    c = dict(A=A, dt=x, Bm=rows[..., :N], Cm=rows[..., N:], u=dy, h0=h0, dt_bias=dt_bias)
+    out = dict(dA=torch.empty((D, N), device="cuda"), ddt=dx, du=torch.empty_like(x), dh0=torch.empty(D, device="cuda"),
+               ddt_bias=torch.empty(D, device="cuda"),
+               **{k: torch.empty((1, T, 1, N), dtype=torch.bfloat16, device="cuda") for k in ("dBm", "dCm")})
+    lh.selective_backward(dy=dy, **c, **out)
+    args = {k: np64(v[:, last]) if k in ("dt", "u", "Bm", "Cm") else np64(v) for k, v in c.items()}
+    ref, mag = ob.selective_grad(np64(dy[:, last]), **args), ob.selective_grad(np64(dy[:, last]), **args, magnitude=True)
+    for k in ("ddt", "du", "dBm", "dCm"):
+        check(out[k][:, last][:, own], ref[k][:, own], mag[k][:, own], 8 * tail + D + N + 128, "bf16", k)
