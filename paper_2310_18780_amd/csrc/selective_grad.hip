@@ -92,10 +92,9 @@ struct Chunk {
 };
 
 // Every load of a chunk starts before the first is used (rows past the last token are its
-// copies, and become zeros in LDS).  The chunk has a token.  Returns whether this thread's
-// steps, inputs, d, B and C are all finite (false, too, where their sum overflows).
+// copies, and become zeros in LDS).  The chunk has a token.
 template <typename T, int NS, int S, bool GATE>
-__device__ __forceinline__ bool load_chunk(const Selective& s, const SelectiveGrads& g,
+__device__ __forceinline__ void load_chunk(const Selective& s, const SelectiveGrads& g,
                                            const Place& p, Chunk<S, NS>& m)
 {
     constexpr int kChunk = chunk_steps(NS), R = kChunk / S;
@@ -127,7 +126,6 @@ __device__ __forceinline__ bool load_chunk(const Selective& s, const SelectiveGr
         rB[i] = pB[j * s.ld_b + n];
         rC[i] = pC[j * s.ld_c + n];
     }
-    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int j = p.wave + i * S;
@@ -140,7 +138,6 @@ __device__ __forceinline__ bool load_chunk(const Selective& s, const SelectiveGr
         if (j >= left) delta = du = d = 0.f;
         // (lanes past the group add nothing to the sums over channels)
         if (!p.own) du = d = 0.f;
-        sum += fabsf(delta) + (fabsf(du) + fabsf(d));
         m.delta[j][p.lane] = delta;
         m.du[j][p.lane] = du;
         m.d[j][p.lane] = d;
@@ -150,13 +147,23 @@ __device__ __forceinline__ bool load_chunk(const Selective& s, const SelectiveGr
         const int e = threadIdx.x + i * kWave * S, j = e / (S * NS), n = e % (S * NS);
         if (e < kChunk * S * NS) {
             const bool in = j < left && n < s.N;
-            const float bv = in ? io_load(&rB[i]) : 0.f, cv = in ? io_load(&rC[i]) : 0.f;
-            m.B[j][n] = bv;
-            m.C[j][n] = cv;
-            sum += fabsf(bv) + fabsf(cv);
+            m.B[j][n] = in ? io_load(&rB[i]) : 0.f;
+            m.C[j][n] = in ? io_load(&rC[i]) : 0.f;
         }
     }
     __syncthreads();
+}
+
+// Whether this thread's share of a chunk is finite (false, too, where its sum overflows).
+template <int S, int NS>
+__device__ __forceinline__ bool finite_share(const Chunk<S, NS>& m)
+{
+    constexpr int kSteps = Chunk<S, NS>::kChunk;
+    float sum = 0.f;
+    for (int e = threadIdx.x; e < kSteps * kWave; e += kWave * S)
+        sum += fabsf((&m.delta[0][0])[e]) + (fabsf((&m.du[0][0])[e]) + fabsf((&m.d[0][0])[e]));
+    for (int e = threadIdx.x; e < kSteps * S * NS; e += kWave * S)
+        sum += fabsf((&m.B[0][0])[e]) + fabsf((&m.C[0][0])[e]);
     return sum < INFINITY;
 }
 
@@ -329,7 +336,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
         if (p.wave == 0) part[s.D * s.N + p.c] = part[s.D * s.N + s.D + p.c] = 0.f;
         return;
     }
-    const bool finite = load_chunk<T, NS, S, GATE>(s, g, p, m);
+    load_chunk<T, NS, S, GATE>(s, g, p, m);
     // Slots past N, steps past the row's tokens and lanes past the group hold zeros and add zeros
     // to the sums, unless an input, or the state that the tokens leave, is not finite: zero times
     // infinity is not zero.  The guarded form of a block leaves them out.  A whole workgroup takes
@@ -337,7 +344,7 @@ __global__ __launch_bounds__(kWave* S) void grad_kernel(Selective s, SelectiveGr
     bool guarded = false;
     if (s.N < NS * S || p.width < kWave) {
         if (p.lane == 0) pp[p.wave][0][0] = 0.f;
-        if (!finite) pp[p.wave][0][0] = 1.f;
+        if (!finite_share(m)) pp[p.wave][0][0] = 1.f;
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < S; ++k) guarded |= pp[k][0][0] != 0.f;
