@@ -125,8 +125,10 @@ __device__ __forceinline__ float sigmoid(float x)
 }
 
 // log(1 + e^x) = max(x, 0) + log(1 + e), e = e^-|x|.  w = 1 + e is rounded; the
-// rounding e - (w - 1) is added back to log w, which leaves a relative error of
-// about 2^-24 also where e is far below 1 (there w = 1 and the term is e).
+// rounding e - (w - 1) is added back to log w, so that nothing of e is lost where it is
+// far below 1 (there w = 1 and the term is e).  What is left is e's own error: its exponent
+// -|x| log2 e is rounded, so the relative error grows with |x|, to at most about
+// (7 + 1.25 |x|) 2^-24 for x < 0 and 7 x 2^-24 above.
 __device__ __forceinline__ float softplus(float x)
 {
     const float e = exp2_fast(-kLog2e * fabsf(x));
