@@ -468,12 +468,15 @@ SelectivePlan selective_plan(int64_t B, int64_t T, int64_t D, int N, int G)
     SelectivePlan p;
     const int64_t tiles = B * group_tiles(D, G) * G;
     // One pass takes about 6 us and 0.1 us a step while the tiles leave the SIMDs waiting
-    // (8 wavefronts to a tile, up to 270 tiles; then in proportion); chunks take 14 us for
-    // two or three launches and, with the SIMDs full, 0.45 ns a step and tile at 16 states.
-    // (T = 2048, D = 2048, 16 states, one pass and chunks: 4 rows 199 and 133 us, 6 rows
-    // 200 and 194, 8 rows 199 and 232; 4 rows of 128 steps 18 and 25 us, 1 row of 256 steps
-    // 30 and 22 us.)
-    const double one = 6.0 + 0.1 * T * (tiles > 270 ? tiles / 270.0 : 1.0);
+    // (8 wavefronts to a tile, up to 270 tiles; then in proportion), from 17 states on, where a
+    // lane or a workgroup holds more of them, 50 + 2.6 N ns; chunks take 14 us for two or three
+    // launches and, with the SIMDs full, 0.45 ns a step and tile at 16 states.
+    // (T = 2048, D = 2048, one pass and chunks: 16 states, 4 rows 199 and 133 us, 6 rows
+    // 200 and 194, 8 rows 199 and 232; 32 states, 4 rows 273 and 190, 8 rows 275 and 328; 64
+    // states, 2 rows 434 and 210, 4 rows 436 and 389; 128 states, 2 rows 786 and 379, 4 rows
+    // 792 and 711.  16 states: 4 rows of 128 steps 18 and 25 us, 1 row of 256 steps 30 and 22.)
+    const double step = N <= 16 ? 0.1 : 0.05 + 0.0026 * N;
+    const double one = 6.0 + step * T * (tiles > 270 ? tiles / 270.0 : 1.0);
     const double cut = 14.0 + 4.5e-4 * T * tiles * (N + 8) / 24;
     // Chunks fill 8192 wavefronts (8 to a SIMD) where they stay 32 steps or longer.
     const int wide = N <= 16 ? 4 : N <= 32 ? 8 : 16;

@@ -59,3 +59,13 @@ def test_rows_far_apart():
     need = lh.selective_backward_workspace_bytes(2, 1, 2048, 16)
     assert lh.lib().lh_selective_backward(ctypes.byref(inputs(2, 1, 2048, 16, **far)), ctypes.byref(g), A + (13 << 40), need,
                                           None) == OVERLAP
+
+
+def test_prompts_of_many_states_are_cut_where_that_is_faster():
+    # 2048 steps and channels, us in one pass and in chunks: 64 states, 4 rows 436 and 389; 128
+    # states, 2 rows 786 and 379, 4 rows 792 and 711; 32 states, 8 rows 275 and 328
+    cut = lambda B, N: lh.selective_workspace_bytes(B, 2048, 2048, N) > 0  # noqa: E731
+    assert cut(4, 64) and cut(2, 128) and cut(4, 128)
+    assert not cut(8, 32) and not cut(8, 64) and not cut(8, 128)
+    # up to 16 states: 4 rows 199 and 133, 8 rows 199 and 232
+    assert cut(4, 16) and not cut(8, 16)
