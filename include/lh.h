@@ -450,12 +450,14 @@ lh_status lh_distill(const float* A, const float* theta, const lh_c32* R, const 
  * element) but for the pairs named below, which may be the same buffer.
  *
  * lengths ([B] int32, or NULL): a right-padded batch; row b has lengths[b] tokens (a
- * value outside [0, T] is taken as the nearer end).  Tokens past them are not read,
- * their outputs and gradients are 0, and they leave the state alone.
+ * value outside [0, T] is taken as the nearer end).  Tokens past them are not read
+ * (the memory must be accessible all the same), their outputs and gradients are 0, and
+ * they leave the state alone.
  *
  * Sums, statistics and states are float32; bfloat16 outputs are rounded once, to
  * nearest even.  Every call gives the same bits for the same inputs.  Sizes that need
- * 2^32 threads or more in one launch return LH_ERR_INVALID_ARG.
+ * 2^32 threads or more in one launch return LH_ERR_INVALID_ARG (layer norm and the
+ * convolution count the launches of their gradients, and a thread for each channel).
  */
 
 /*
@@ -602,7 +604,10 @@ typedef struct lh_selective_grads {
     float* ddt_bias; /* out [D], or NULL */
 } lh_selective_grads;
 
-/* Workspace bytes of lh_selective_backward; (size_t)-1 for invalid sizes. */
+/* Workspace bytes of lh_selective_backward; (size_t)-1 for invalid sizes.  About
+ * 5/16 B T D N bytes up to 32 states and 1/2 B T D N beyond: states and gradients of
+ * each chunk, and partial sums (16 x 4096 x 2048: 0.7 GB with 16 states, 4.3 GB with 64).
+ */
 size_t lh_selective_backward_workspace_bytes(int64_t B, int64_t T, int64_t D, int64_t N,
                                              int64_t G);
 

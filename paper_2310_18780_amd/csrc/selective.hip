@@ -16,8 +16,8 @@
 // Bound by the VALU: per state and step two products, two multiply-adds (4 cycles each)
 // and an exponential (8 cycles), beside about 38 instructions a channel and step for
 // softplus, silu, the sum of the parts and conversions.  16 x 4096 x 2048 bfloat16 with 16
-// states: 568 us (1.9 TB/s; vector issue 0.73 of the time at 2.4 GHz, and the clock is
-// nearer 2.0 under this load).  What brought it there from 2047 us: loads not converted
+// states: 565 us (1.9 TB/s; vector issue 0.84 of the time at 2.4 GHz; the clock is lower in
+// the first 25 ms of load, up to 760 us).  What brought it there from 2047 us: loads not converted
 // where they are issued (784), 32-bit byte offsets from a uniform row and no branch for
 // the row's end inside a tile (629), twice the wavefronts with half the states (570).
 // Taken back: two tiles' buffers and one barrier a tile (LDS leaves fewer workgroups,
@@ -28,7 +28,7 @@
 // pass forms each chunk's end state from zero and its sum of steps (a chunk's decay is
 // e^(A sum delta), one exponential), a carry turns end states into entry states, and
 // the output pass starts every chunk from its own: 0.83 times the output pass's work
-// again, for all SIMDs (1 x 65536 x 1024 float32: 479 us, the passes 197 and 264).
+// again, for all SIMDs (1 x 65536 x 1024 float32: 477 us, the passes 195 and 262).
 //
 // Single tokens: four states of a (batch row, channel) to a lane, y summed over the
 // row's lanes; bound by the state, read once and written once (64 x 2048, 16 states, 18
@@ -41,7 +41,7 @@ namespace {
 constexpr int kSteps = 16;  // steps of a tile
 // Up to this many chunks a launch for the carry costs more than carrying in every chunk
 // (1 row of 512 steps, D = 768: 18.9 us against 21.1; of 2048 steps, 64 chunks, 69.7
-// against 52.5).
+// against 52.5; between 16 and 64 chunks it was not measured).
 constexpr int64_t kFewChunks = 16;
 
 // f with n as a constant, 0 <= n <= MOST (n < 0 is 0).

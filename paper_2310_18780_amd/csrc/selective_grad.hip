@@ -23,10 +23,14 @@
 // lanes each), about two instructions a value instead of six adds, and leave as
 // partial rows per tile; a last launch adds the tiles of a group in a fixed order.
 //
+// Steps past a row's tokens and slots without a state are left out of a block by its guarded
+// form: the block that the tokens end in, and every block of a chunk that holds a value that is
+// not finite while slots or lanes are empty.  Chunks without tokens only write zeros.
+//
 // Bound by the VALU: per state and step 7 instructions (one an exponential) in the first
 // pass and 28 in the main one (two exponentials, 5 of them folds).  4 x 4096 x 2048
-// bfloat16 with 16 states: 820 us (225 the first pass, 30 the carry, 615 the main pass, 19
-// and 9 the sums, traced; vector issue 0.70 of both passes at 2.4 GHz).  With each load of a chunk
+// bfloat16 with 16 states: 820 us (traced 200 the first pass, 29 the carry, 562 the main pass,
+// 19 and 9 the sums; vector issue 0.77 of both passes at 2.4 GHz).  With each load of a chunk
 // waited for in turn it took 1425 us.
 #include "selective.hpp"
 

@@ -18,7 +18,8 @@
 // A run's sums for dw and dbias stay in registers; the workgroup's runs over the
 // same channels are added in LDS, and a second launch adds the workgroups' rows in a
 // fixed order (16 x 2048 x 768 float32, rows 2 x 768 apart: 71 us for 302 MB, 84 us
-// without the inputs ahead; 64 x 2048 x 2048 bfloat16 361 us, 4.5 TB/s, against 554).
+// without the inputs ahead; 57 us where the call before read the same inputs, part of which
+// then lie in the 256 MB cache; 64 x 2048 x 2048 bfloat16 361 us, 4.5 TB/s, against 554).
 #include "short_conv.hpp"
 
 #include "block_ops.hpp"
@@ -27,7 +28,7 @@ namespace lh {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int64_t kThreads = 1 << 16;  // one wavefront per SIMD  
+constexpr int64_t kThreads = 1 << 16;  // one wavefront per SIMD
 
 constexpr int kAhead = 4;  // steps whose inputs are in flight while as many are computed
 
@@ -341,8 +342,9 @@ struct GradShape {
 GradShape grad_shape(int64_t B, int64_t T, int64_t D, int64_t K, int V)
 {
     // Runs of up to 64 steps: 64 where that leaves three workgroups to a CU, else the
-    // longest up to 32 that leaves one (16 x 2048 x 768: float32 runs of 32 and 64 steps 58
-    // and 60 us; 2 x 2048 x 2048 bfloat16 runs of 16 and 8 steps 24 and 27 us).
+    // longest up to 32 that leaves one (on the inputs of the call before, 16 x 2048 x 768:
+    // float32 runs of 32 and 64 steps 58 and 60 us; 2 x 2048 x 2048 bfloat16 runs of 16 and 8
+    // steps 24 and 27 us).
     const int64_t cols = (D + V - 1) / V, least = K <= 5 ? 4 : 8;
     GradShape s;
     s.tiles = (cols + kWave - 1) / kWave;
