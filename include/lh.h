@@ -553,7 +553,9 @@ lh_status lh_short_conv_backward(const void* dy, const void* x, int64_t ld_x, co
  *   x[n]  = exp(delta A[c,n]) x[n] + delta Bm[b,t,g,n] u[b,t,c]
  *   y     = sum_n Cm[b,t,g,n] x[n] + h0[c] u[b,t,c],  times z sigmoid(z) where z is given
  *
- * (the output reads the state after the update, unlike lh_step's.)
+ * (the output reads the state after the update, unlike lh_step's.)  A <= 0, -infinity among
+ * them: a state that decays, or with A = 0 a sum.  Prompts and gradients multiply decays over
+ * up to a whole prompt, so with A > 0 results are only right while e^(A sum delta) is finite.
  */
 typedef struct lh_selective_inputs {
     const float* A;         /* [D, N] */
