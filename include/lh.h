@@ -618,6 +618,192 @@ size_t lh_selective_backward_workspace_bytes(int64_t B, int64_t T, int64_t D, in
 lh_status lh_selective_backward(const lh_selective_inputs* in, const lh_selective_grads* grads,
                                 void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The ends of a recurrent language model and its gated recurrence: token embedding, a
+ * gated linear recurrence, distillation from a teacher's top logits, and the verification
+ * of drafted tokens.  Rows, lengths, overlaps, types and the order of sums are as said at
+ * the selective block above.  Token ids are int32.
+ */
+
+/* The gated recurrence keeps the state before every LH_GATED_MARK-th token for its gradient. */
+#define LH_GATED_MARK 64
+
+/*
+ * Gated linear recurrence.  Per batch row and channel c:
+ *
+ *   f = sigmoid(r[b,t,c] + r_bias[c]),  p = sigmoid(i[b,t,c] + i_bias[c])
+ *   a = exp(-rate[c] f),  h <- a h + sqrt(1 - a^2) p u[b,t,c]
+ *   y = h,  times z sigmoid(z) where z is given
+ *
+ * rate >= 0 and finite: how fast a channel can forget (0: it holds its state; below 0 the
+ * results are NaN).
+ */
+typedef struct lh_gated_inputs {
+    const float* rate;      /* [D] */
+    const float* r_bias;    /* [D] or NULL (0) */
+    const float* i_bias;    /* [D] or NULL (0) */
+    const void* r;          /* [B, T, D] (io_dtype), rows ld_r apart */
+    const void* i;          /* [B, T, D] (io_dtype), rows ld_i apart */
+    const void* u;          /* [B, T, D] (io_dtype), rows ld_u apart */
+    const void* z;          /* [B, T, D] (io_dtype), rows ld_z apart; NULL: no gate */
+    const int32_t* lengths; /* [B] or NULL */
+    int64_t ld_r, ld_i, ld_u, ld_z;
+    int64_t B, T, D;        /* B >= 1, T >= 0, D >= 1 */
+    lh_dtype io_dtype;
+} lh_gated_inputs;
+
+/* Workspace bytes of lh_gated_prefill; (size_t)-1 for invalid sizes. */
+size_t lh_gated_workspace_bytes(int64_t B, int64_t T, int64_t D);
+
+/*
+ * The recurrence over a prompt.
+ *   resume    : start from the state (else from zero, and the state is not read)
+ *   state     : in/out [B, D] float32, after each row's last token
+ *   y         : out [B, T, D] (io_dtype)
+ *   marks     : out [B, ceil(T / LH_GATED_MARK), D] float32, the state before the tokens 0,
+ *               LH_GATED_MARK, 2 LH_GATED_MARK, ..., which the gradient takes; not written
+ *               where a row has no such token; NULL where not needed
+ *   workspace : lh_gated_workspace_bytes bytes, 256-byte aligned (NULL allowed when that
+ *               is 0)
+ * One kernel launch, or two where the prompt is cut into chunks.
+ */
+lh_status lh_gated_prefill(const lh_gated_inputs* in, int resume, float* state, void* y,
+                           float* marks, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token per batch row (T = 1, lengths NULL): y_t [B, D] and the state in place.  One
+ * kernel launch; no workspace. */
+lh_status lh_gated_step(const lh_gated_inputs* in, float* state, void* y_t, void* stream);
+
+/* What lh_gated_backward takes and gives beside the inputs. */
+typedef struct lh_gated_grads {
+    const void* dy;     /* [B, T, D] (io_dtype): the gradient of y */
+    const float* marks; /* what lh_gated_prefill left, with resume or without */
+    const float* dlast; /* [B, D]: the gradient of the state after the prompt; NULL: 0 */
+    void* dr;           /* out [B, T, D] (io_dtype) */
+    void* di;           /* out [B, T, D] (io_dtype) */
+    void* du;           /* out [B, T, D] (io_dtype) */
+    void* dz;           /* out [B, T, D] (io_dtype); NULL where z is NULL, and only there */
+    float* drate;       /* out [D]; 0 where rate is 0 (the slope of the square root there
+                           has no bound) */
+    float* dr_bias;     /* out [D], or NULL */
+    float* di_bias;     /* out [D], or NULL */
+    float* dfirst;      /* out [B, D]: the gradient of the state before the prompt; or NULL */
+} lh_gated_grads;
+
+/* Workspace bytes of lh_gated_backward; (size_t)-1 for invalid sizes. */
+size_t lh_gated_backward_workspace_bytes(int64_t B, int64_t T, int64_t D);
+
+/* Gradients of lh_gated_prefill.  workspace as there. */
+lh_status lh_gated_backward(const lh_gated_inputs* in, const lh_gated_grads* grads,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Embedding: y[k] = scale W[ids[k]], in float32, rounded once.
+ *
+ *   W      : [V, D] (table_dtype);  ids : [n] int32
+ *   y      : out [n, D] (io_dtype)
+ *   n >= 0, V >= 1, D >= 1; n and V < 2^31; each type LH_F32 or LH_BF16
+ * An id outside [0, V) gives a row of zeros.  One kernel launch; no workspace.
+ */
+lh_status lh_embed(const void* W, const int32_t* ids, int64_t n, int64_t V, int64_t D,
+                   lh_dtype table_dtype, lh_dtype io_dtype, float scale, void* y, void* stream);
+
+/* Workspace bytes of lh_embed_backward (16 n and up to n D / 2); (size_t)-1 for invalid sizes. */
+size_t lh_embed_backward_workspace_bytes(int64_t n, int64_t V, int64_t D);
+
+/*
+ * The table's gradient: dW[v] = scale sum over k with ids[k] = v of dy[k], the tokens sorted
+ * by id and added in a fixed order.
+ *
+ *   dy         : [n, D] (io_dtype);  dW : out [V, D] float32
+ *   accumulate : dW is added to (rows without a token are not touched); else every row is
+ *                written
+ * Ids outside [0, V) take no part.  workspace as in lh_gated_prefill.
+ */
+lh_status lh_embed_backward(const void* dy, const int32_t* ids, int64_t n, int64_t V, int64_t D,
+                            lh_dtype io_dtype, float scale, int accumulate, float* dW,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Largest number of a teacher's logits per row. */
+#define LH_DISTILL_MAX_TOP 1024
+
+/* Workspace bytes of lh_distill_logits; (size_t)-1 for invalid sizes. */
+size_t lh_distill_logits_workspace_bytes(int64_t rows, int64_t V, int64_t K);
+
+/*
+ * Distillation from a teacher's top logits.  Per row, with t = values / tau over the slots
+ * k whose id is in [0, V) and whose value is not -infinity, and x = logits / tau:
+ *
+ *   p = softmax(t),  q = softmax(x)
+ *   loss = scale tau^2 sum_k p_k (log p_k - log q[id_k])
+ *   dlogits[j] = scale tau (q[j] - sum of p_k with id_k = j)
+ *   lse = log sum_j exp(x_j)
+ *
+ * (an id given twice counts twice).  A row without such a slot, or whose scale is 0, has
+ * loss and gradient 0 and its logits are not read (the memory must be accessible all the
+ * same); its lse is 0.  A row whose logits are all -infinity has q = 0.
+ *
+ *   logits  : [rows, V] (io_dtype), rows ld_logits apart
+ *   values  : [rows, K] float32;  ids : [rows, K] int32
+ *   scale   : [rows] float32, or NULL (1)
+ *   rows >= 0, V >= 1, 1 <= K <= LH_DISTILL_MAX_TOP, tau > 0 and finite; V < 2^31
+ *   loss    : out [rows] float32
+ *   lse     : out [rows] float32, which lh_distill_logits_backward takes; or NULL
+ *   dlogits : out [rows, V] (io_dtype), rows ld_dlogits apart, the gradient of the sum of
+ *             the losses; or NULL.  It may be the buffer of logits (with the same ld).
+ *   workspace as in lh_gated_prefill
+ */
+lh_status lh_distill_logits(const void* logits, int64_t ld_logits, const float* values,
+                            const int32_t* ids, const float* scale, int64_t rows, int64_t V,
+                            int64_t K, lh_dtype io_dtype, float tau, float* loss, float* lse,
+                            void* dlogits, int64_t ld_dlogits, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* The gradient for an upstream gradient dloss [rows] (float32) of the losses: dlogits of
+ * lh_distill_logits times dloss, from its lse.  One kernel launch; no workspace. */
+lh_status lh_distill_logits_backward(const float* dloss, const void* logits, int64_t ld_logits,
+                                     const float* values, const int32_t* ids, const float* scale,
+                                     const float* lse, int64_t rows, int64_t V, int64_t K,
+                                     lh_dtype io_dtype, float tau, void* dlogits,
+                                     int64_t ld_dlogits, void* stream);
+
+/* Largest number of drafted tokens per row. */
+#define LH_VERIFY_MAX_DRAFT 64
+
+/* Workspace bytes of lh_verify_draft; (size_t)-1 for invalid sizes. */
+size_t lh_verify_draft_workspace_bytes(int64_t B, int64_t K, int64_t V);
+
+/*
+ * Verification of drafted tokens: tokens distributed as the target's, of which as many of
+ * the drafted ones as the given random numbers accept.  Row b has n = lengths[b] drafted
+ * tokens t_0 .. t_(n-1) (n outside [0, K] is taken as the nearer end), drawn from q_i =
+ * draft_p[b, i]; p_i = target_p[b, i] are the target's probabilities after i of them.
+ *
+ *   token i is accepted while u[b,i] q_i(t_i) < p_i(t_i);  m = the first that is not, or n
+ *   w = max(p_m - q_m, 0) where m < n, p_n where m = n
+ *   next token = the lowest j with  w_0 + ... + w_j > u_last[b] (w_0 + ... + w_(V-1))
+ *
+ * Differences and sums are float64.  A drafted token outside [0, V) is not accepted (and
+ * with draft_p = NULL takes nothing from w).  Entries of w that are negative or NaN count
+ * as 0; where nothing of w is left, w = p_m; where nothing of that is left either, the next
+ * token is -1.  Probabilities need not sum to 1; they must be finite.
+ *
+ *   drafted  : [B, K] int32;  lengths : [B] int32 or NULL (K)
+ *   draft_p  : [B, K, V] (io_dtype), rows ld_draft apart; NULL: the draft is certain of its
+ *              tokens (q_i is 1 at t_i and 0 elsewhere)
+ *   target_p : [B, K + 1, V] (io_dtype), rows ld_target apart
+ *   u        : [B, K] float32;  u_last : [B] float32, in [0, 1)
+ *   B >= 1, 1 <= K <= LH_VERIFY_MAX_DRAFT, V >= 1; V < 2^31
+ *   accepted : out [B] int32, m
+ *   tokens   : out [B, K + 1] int32: the m accepted tokens, the next token, then -1
+ *   workspace as in lh_gated_prefill
+ */
+lh_status lh_verify_draft(const int32_t* drafted, const int32_t* lengths, const void* draft_p,
+                          int64_t ld_draft, const void* target_p, int64_t ld_target,
+                          const float* u, const float* u_last, int64_t B, int64_t K, int64_t V,
+                          lh_dtype io_dtype, int32_t* accepted, int32_t* tokens, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

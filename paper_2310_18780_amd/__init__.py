@@ -18,6 +18,13 @@ The selective block beside it (prompts, single tokens, gradients):
     short_conv_prefill, short_conv_step, short_conv_backward
     selective_prefill, selective_step, selective_backward
 
+The gated recurrence and the two ends of a language model:
+
+    gated_prefill, gated_step, gated_backward
+    embed, embed_backward
+    distill_logits, distill_logits_backward
+    verify_draft
+
 ``lam``, ``R``: complex64 ``[D, d]``; ``h0``: float32 ``[D]``; ``u``, ``y``:
 float32 or bfloat16 ``[B, T, D]``; ``state``: complex64 ``[B, D, d]``;
 ``u_t``, ``y_t``: ``[B, D]``.
@@ -66,6 +73,20 @@ __all__ = [
     "selective_step",
     "selective_backward_workspace_bytes",
     "selective_backward",
+    "GATED_MARK",
+    "gated_workspace_bytes",
+    "gated_prefill",
+    "gated_step",
+    "gated_backward_workspace_bytes",
+    "gated_backward",
+    "embed",
+    "embed_backward_workspace_bytes",
+    "embed_backward",
+    "distill_logits_workspace_bytes",
+    "distill_logits",
+    "distill_logits_backward",
+    "verify_draft_workspace_bytes",
+    "verify_draft",
     "STATUS",
 ]
 
@@ -80,6 +101,8 @@ PLAN_MFMA = -1
 PLAN_MFMA_SEG = -2
 # scratch that lh_prefill_noalloc holds per GPU
 NOALLOC_SCRATCH_BYTES = 64 << 20
+# tokens between the states that gated_prefill leaves for gated_backward
+GATED_MARK = 64
 STATUS = {
     0: "LH_OK",
     1: "LH_ERR_INVALID_ARG",
@@ -104,6 +127,17 @@ class _SelectiveInputs(ctypes.Structure):
 
 class _SelectiveGrads(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("dy", "ddt", "du", "dz", "dBm", "dCm", "dA", "dh0", "ddt_bias")]
+
+
+class _GatedInputs(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("rate", "r_bias", "i_bias", "r", "i", "u", "z", "lengths")]
+                + [(k, ctypes.c_int64) for k in ("ld_r", "ld_i", "ld_u", "ld_z", "B", "T", "D")]
+                + [("io_dtype", ctypes.c_int)])
+
+
+class _GatedGrads(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("dy", "marks", "dlast", "dr", "di", "du", "dz", "drate", "dr_bias",
+                                               "di_bias", "dfirst")]
 
 
 class LHError(RuntimeError):
@@ -201,6 +235,22 @@ def lib() -> ctypes.CDLL:
     L.lh_selective_step.restype = ci
     L.lh_selective_backward.argtypes = [vp, vp, vp, sz, vp]
     L.lh_selective_backward.restype = ci
+    cf = ctypes.c_float
+    for name in ("lh_gated_workspace_bytes", "lh_gated_backward_workspace_bytes", "lh_embed_backward_workspace_bytes",
+                 "lh_distill_logits_workspace_bytes", "lh_verify_draft_workspace_bytes"):
+        getattr(L, name).argtypes = [i64, i64, i64]
+        getattr(L, name).restype = sz
+    for name, args in (
+            ("lh_gated_prefill", [vp, ci, vp, vp, vp, vp, sz, vp]),
+            ("lh_gated_step", [vp, vp, vp, vp]),
+            ("lh_gated_backward", [vp, vp, vp, sz, vp]),
+            ("lh_embed", [vp, vp, i64, i64, i64, ci, ci, cf, vp, vp]),
+            ("lh_embed_backward", [vp, vp, i64, i64, i64, ci, cf, ci, vp, vp, sz, vp]),
+            ("lh_distill_logits", [vp, i64, vp, vp, vp, i64, i64, i64, ci, cf, vp, vp, vp, i64, vp, sz, vp]),
+            ("lh_distill_logits_backward", [vp, vp, i64, vp, vp, vp, vp, i64, i64, i64, ci, cf, vp, i64, vp]),
+            ("lh_verify_draft", [vp, vp, vp, i64, vp, i64, vp, vp, i64, i64, i64, ci, vp, vp, vp, sz, vp])):
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = ci
     _lib = L
     return L
 
@@ -766,3 +816,197 @@ def selective_backward(dy, A, dt, Bm, Cm, u, dA, ddt, dBm, dCm, du, h0=None, dh0
     workspace, ws_ptr, ws_len = _scratch(selective_backward_workspace_bytes(B, T, D, N, G), workspace,
                                          u.device, stream)
     _check(lib().lh_selective_backward(ctypes.byref(s), ctypes.byref(g), ws_ptr, ws_len, handle))
+
+
+# ---- the gated recurrence
+
+def _gated_args(rate, r, i, u, r_bias, i_bias, z, lengths, lead):
+    torch = _torch_loaded()
+    D, = rate.shape
+    dtype, k, rows = u.dtype, len(lead), (*lead, D)
+    _need(rate, "rate", torch.float32, (D,))
+    ld_r = _need_rows(r, "r", dtype, rows, k, D)
+    ld_i = _need_rows(i, "i", dtype, rows, k, D)
+    ld_u = _need_rows(u, "u", dtype, rows, k, D)
+    ld_z = pz = pr = pi = pl = None
+    if z is not None:
+        ld_z, pz = _need_rows(z, "z", dtype, rows, k, D), z.data_ptr()
+    if r_bias is not None:
+        _need(r_bias, "r_bias", torch.float32, (D,))
+        pr = r_bias.data_ptr()
+    if i_bias is not None:
+        _need(i_bias, "i_bias", torch.float32, (D,))
+        pi = i_bias.data_ptr()
+    if lengths is not None:
+        _need_lengths(lengths, lead[0])
+        pl = lengths.data_ptr()
+    return _GatedInputs(rate.data_ptr(), pr, pi, r.data_ptr(), i.data_ptr(), u.data_ptr(), pz, pl, ld_r, ld_i, ld_u,
+                        ld_z or 0, lead[0], lead[1] if k > 1 else 1, D, _io_dtype(u))
+
+
+def gated_workspace_bytes(B: int, T: int, D: int) -> int:
+    return _block_bytes("lh_gated_workspace_bytes", B, T, D)
+
+
+def gated_prefill(rate, r, i, u, state, y, r_bias=None, i_bias=None, z=None, lengths=None, resume: bool = False,
+                  marks=None, workspace=None, stream=None) -> None:
+    """Gated linear recurrence over a prompt (``lh_gated_prefill``): ``r``, ``i``, ``u``, ``z``
+    ``[B, T, D]`` (all may be slices of rows), ``rate``, ``r_bias``, ``i_bias`` ``[D]`` and
+    ``state [B, D]`` float32; writes ``y [B, T, D]`` and the state, which the prompt continues
+    from where ``resume``.  ``marks [B, ceil(T / GATED_MARK), D]`` float32 receives the states
+    that ``gated_backward`` takes."""
+    B, T = u.shape[:2]
+    s = _gated_args(rate, r, i, u, r_bias, i_bias, z, lengths, (B, T))
+    _need(state, "state", _torch.float32, (B, s.D))
+    _need(y, "y", u.dtype, (B, T, s.D))
+    if marks is not None:
+        _need(marks, "marks", _torch.float32, (B, -(-T // GATED_MARK), s.D))
+    handle = _handle(u, stream)
+    workspace, ws_ptr, ws_len = _scratch(gated_workspace_bytes(B, T, s.D), workspace, u.device, stream)
+    _check(lib().lh_gated_prefill(ctypes.byref(s), resume, state.data_ptr(), y.data_ptr(), _ptr(marks), ws_ptr, ws_len,
+                                  handle))
+
+
+def gated_step(rate, r_t, i_t, u_t, state, y_t, r_bias=None, i_bias=None, z=None, stream=None) -> None:
+    """One token per row (``lh_gated_step``): ``r_t``, ``i_t``, ``u_t``, ``z``, ``y_t`` ``[B, D]``,
+    ``state`` in place."""
+    B = u_t.shape[0]
+    s = _gated_args(rate, r_t, i_t, u_t, r_bias, i_bias, z, None, (B,))
+    _need(state, "state", _torch.float32, (B, s.D))
+    _need(y_t, "y_t", u_t.dtype, (B, s.D))
+    _check(lib().lh_gated_step(ctypes.byref(s), state.data_ptr(), y_t.data_ptr(), _handle(u_t, stream)))
+
+
+def gated_backward_workspace_bytes(B: int, T: int, D: int) -> int:
+    return _block_bytes("lh_gated_backward_workspace_bytes", B, T, D)
+
+
+def gated_backward(dy, rate, r, i, u, marks, drate, dr, di, du, r_bias=None, dr_bias=None, i_bias=None, di_bias=None,
+                   z=None, dz=None, lengths=None, dlast=None, dfirst=None, workspace=None, stream=None) -> None:
+    """Gradients of ``gated_prefill`` (``lh_gated_backward``) from its inputs, the ``marks`` it
+    left and ``dy [B, T, D]``.  ``dlast [B, D]`` is the gradient of the state after the prompt
+    (None: 0), ``dfirst [B, D]`` receives that of the state before it."""
+    torch = _torch_loaded()
+    B, T = u.shape[:2]
+    s = _gated_args(rate, r, i, u, r_bias, i_bias, z, lengths, (B, T))
+    D, g, f32 = s.D, _GatedGrads(), torch.float32
+    for name, t, dtype, shape in (
+            ("dy", dy, u.dtype, (B, T, D)), ("marks", marks, f32, (B, -(-T // GATED_MARK), D)),
+            ("dlast", dlast, f32, (B, D)), ("dr", dr, u.dtype, (B, T, D)), ("di", di, u.dtype, (B, T, D)),
+            ("du", du, u.dtype, (B, T, D)), ("dz", dz, u.dtype, (B, T, D)), ("drate", drate, f32, (D,)),
+            ("dr_bias", dr_bias, f32, (D,)), ("di_bias", di_bias, f32, (D,)), ("dfirst", dfirst, f32, (B, D))):
+        if t is not None:
+            _need(t, name, dtype, shape)
+            setattr(g, name, t.data_ptr())
+        elif name in ("dy", "marks", "dr", "di", "du", "drate"):
+            raise TypeError(f"{name} must be a torch.Tensor")
+    handle = _handle(u, stream)
+    workspace, ws_ptr, ws_len = _scratch(gated_backward_workspace_bytes(B, T, D), workspace, u.device, stream)
+    _check(lib().lh_gated_backward(ctypes.byref(s), ctypes.byref(g), ws_ptr, ws_len, handle))
+
+
+# ---- the ends of a language model
+
+def embed(W, ids, y, scale: float = 1.0, stream=None) -> None:
+    """Rows of the table ``W [V, D]`` times ``scale`` (``lh_embed``): ``y [*ids.shape, D]`` for
+    int32 ``ids``; zeros where an id is outside the table.  ``W`` and ``y`` may differ in type."""
+    torch = _torch_loaded()
+    V, D = W.shape
+    _need(W, "W", W.dtype, (V, D))
+    _need(ids, "ids", torch.int32, ids.shape)
+    _need(y, "y", y.dtype, (*ids.shape, D))
+    _check(lib().lh_embed(W.data_ptr(), ids.data_ptr(), ids.numel(), V, D, _io_dtype(W), _io_dtype(y), scale,
+                          y.data_ptr(), _handle(y, stream)))
+
+
+def embed_backward_workspace_bytes(n: int, V: int, D: int) -> int:
+    return _block_bytes("lh_embed_backward_workspace_bytes", n, V, D)
+
+
+def embed_backward(dy, ids, dW, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None) -> None:
+    """Gradient of ``embed`` (``lh_embed_backward``): ``dW [V, D]`` float32, written, or added to
+    where ``accumulate``, from ``dy [*ids.shape, D]``."""
+    torch = _torch_loaded()
+    V, D = dW.shape
+    _need(dW, "dW", torch.float32, (V, D))
+    _need(ids, "ids", torch.int32, ids.shape)
+    _need(dy, "dy", dy.dtype, (*ids.shape, D))
+    n = ids.numel()
+    handle = _handle(dy, stream)
+    workspace, ws_ptr, ws_len = _scratch(embed_backward_workspace_bytes(n, V, D), workspace, dy.device, stream)
+    _check(lib().lh_embed_backward(dy.data_ptr(), ids.data_ptr(), n, V, D, _io_dtype(dy), scale, accumulate,
+                                   dW.data_ptr(), ws_ptr, ws_len, handle))
+
+
+def _distill_args(logits, values, ids, scale, dlogits):
+    torch = _torch_loaded()
+    rows, V = logits.shape
+    K = values.shape[-1]
+    ld = _need_rows(logits, "logits", logits.dtype, (rows, V), 1, V)
+    _need(values, "values", torch.float32, (rows, K))
+    _need(ids, "ids", torch.int32, (rows, K))
+    if scale is not None:
+        _need(scale, "scale", torch.float32, (rows,))
+    ld_d = 0 if dlogits is None else _need_rows(dlogits, "dlogits", logits.dtype, (rows, V), 1, V)
+    return rows, V, K, ld, ld_d, _io_dtype(logits)
+
+
+def distill_logits_workspace_bytes(rows: int, V: int, K: int) -> int:
+    return _block_bytes("lh_distill_logits_workspace_bytes", rows, V, K)
+
+
+def distill_logits(logits, values, ids, loss, dlogits=None, lse=None, scale=None, tau: float = 1.0, workspace=None,
+                   stream=None) -> None:
+    """Distillation from a teacher's top logits (``lh_distill_logits``): ``values``, ``ids``
+    ``[rows, K]`` float32 and int32, ``logits [rows, V]`` (rows may lie apart); writes
+    ``loss [rows]``, where given the gradient ``dlogits`` of the losses' sum (it may be
+    ``logits`` itself) and ``lse [rows]``, which ``distill_logits_backward`` takes.  ``scale
+    [rows]`` multiplies each row's loss; rows of scale 0 take no part."""
+    rows, V, K, ld, ld_d, io = _distill_args(logits, values, ids, scale, dlogits)
+    for name, t in (("loss", loss), ("lse", lse)):
+        if t is not None or name == "loss":
+            _need(t, name, _torch.float32, (rows,))
+    handle = _handle(logits, stream)
+    workspace, ws_ptr, ws_len = _scratch(distill_logits_workspace_bytes(rows, V, K), workspace, logits.device, stream)
+    _check(lib().lh_distill_logits(logits.data_ptr(), ld, values.data_ptr(), ids.data_ptr(), _ptr(scale), rows, V, K, io,
+                                   tau, loss.data_ptr(), _ptr(lse), _ptr(dlogits), ld_d, ws_ptr, ws_len, handle))
+
+
+def distill_logits_backward(dloss, logits, values, ids, lse, dlogits, scale=None, tau: float = 1.0, stream=None) -> None:
+    """Gradient of ``distill_logits`` for an upstream gradient ``dloss [rows]`` of its losses
+    (``lh_distill_logits_backward``)."""
+    if dlogits is None:
+        raise TypeError("dlogits must be a torch.Tensor")
+    rows, V, K, ld, ld_d, io = _distill_args(logits, values, ids, scale, dlogits)
+    _need(dloss, "dloss", _torch.float32, (rows,))
+    _need(lse, "lse", _torch.float32, (rows,))
+    _check(lib().lh_distill_logits_backward(dloss.data_ptr(), logits.data_ptr(), ld, values.data_ptr(), ids.data_ptr(),
+                                            _ptr(scale), lse.data_ptr(), rows, V, K, io, tau, dlogits.data_ptr(), ld_d,
+                                            _handle(logits, stream)))
+
+
+def verify_draft_workspace_bytes(B: int, K: int, V: int) -> int:
+    return _block_bytes("lh_verify_draft_workspace_bytes", B, K, V)
+
+
+def verify_draft(drafted, target_p, u, u_last, accepted, tokens, draft_p=None, lengths=None, workspace=None,
+                 stream=None) -> None:
+    """Verification of drafted tokens (``lh_verify_draft``): ``drafted [B, K]`` int32 against
+    ``target_p [B, K + 1, V]``, with the draft's own probabilities ``draft_p [B, K, V]`` (None: it
+    was certain; rows of both may lie apart) and random numbers ``u [B, K]``, ``u_last [B]`` in
+    [0, 1); writes ``accepted [B]`` and ``tokens [B, K + 1]`` (the accepted, the next, then -1)."""
+    torch = _torch_loaded()
+    B, K = drafted.shape
+    V, dtype, i32, f32 = target_p.shape[-1], target_p.dtype, torch.int32, torch.float32
+    _need(drafted, "drafted", i32, (B, K))
+    ld_t = _need_rows(target_p, "target_p", dtype, (B, K + 1, V), 2, V)
+    ld_d = 0 if draft_p is None else _need_rows(draft_p, "draft_p", dtype, (B, K, V), 2, V)
+    _need_lengths(lengths, B)
+    for name, t, want, shape in (("u", u, f32, (B, K)), ("u_last", u_last, f32, (B,)), ("accepted", accepted, i32, (B,)),
+                                 ("tokens", tokens, i32, (B, K + 1))):
+        _need(t, name, want, shape)
+    handle = _handle(target_p, stream)
+    workspace, ws_ptr, ws_len = _scratch(verify_draft_workspace_bytes(B, K, V), workspace, target_p.device, stream)
+    _check(lib().lh_verify_draft(drafted.data_ptr(), _ptr(lengths), _ptr(draft_p), ld_d, target_p.data_ptr(), ld_t,
+                                 u.data_ptr(), u_last.data_ptr(), B, K, V, _io_dtype(target_p), accepted.data_ptr(),
+                                 tokens.data_ptr(), ws_ptr, ws_len, handle))

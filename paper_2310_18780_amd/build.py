@@ -17,7 +17,8 @@ LIB = os.path.join(HERE, "liblh.so")
 SOURCES = ["lh_api.cpp", "prefill_mfma_f32.hip", "prefill_mfma_bf16.hip", "prefill_mfma.hip", "decode.hip",
            "prefill.hip", "prefill_fft.hip", "multihead.hip", "distill.hip", "companion.hip",
            "block_api.cpp", "block_ops.hip", "norm.hip", "short_conv.hip", "selective.hip",
-           "selective_grad.hip"]
+           "selective_grad.hip", "model_api.cpp", "gated.hip", "gated_grad.hip", "embed.hip", "embed_grad.hip",
+           "distill_logits.hip", "verify.hip"]
 
 # -packed-fp32-ops: no v_pk_{add,mul,fma}_f32 in the generated code (the host
 # pass warns that it does not know the feature; that is harmless).

@@ -1,0 +1,451 @@
+// Gradient of the embedding's table: dW[v] = scale sum over the tokens k of id v of dy[k].
+//
+// The tokens are sorted by id (a stable counting sort, digit by digit, from the least), so
+// that a row's tokens lie side by side in the order of their positions and their sum has the
+// same bits on every call.  Then a workgroup takes a window of sorted tokens and walks it with
+// its columns in registers: what begins and ends in the window is stored, what crosses a
+// border goes to the workspace (at most one run enters and one leaves a window), and a last
+// launch adds those, window by window.  Rows without a token are zeros, which further
+// workgroups of the first launch write while the sort runs.
+//
+// Bound by memory: n rows of dy are read, V rows of dW written (those with tokens twice),
+// beside launches of a few microseconds each.
+#include "embed.hpp"
+
+#include "block_ops.hpp"
+
+namespace lh {
+namespace {
+
+constexpr int kSortBlock = 1024;
+constexpr int kSortWaves = kSortBlock / kWave;
+constexpr int kMaxBits = 9, kMaxDigits = 1 << kMaxBits;
+constexpr int64_t kSmall = 4096;  // tokens that one workgroup sorts in LDS
+constexpr int kFillBlocks = 2048;
+
+// The sort key of an id: ids outside the table come last and take no part.
+__device__ __forceinline__ uint32_t key_of(int id, uint32_t V)
+{
+    return uint32_t(id) < V ? uint32_t(id) : V;
+}
+
+// Zeros of dW by the workgroups from `first` on.
+__device__ __forceinline__ void fill_zeros(float* dW, int64_t count, int64_t first)
+{
+    if (!dW) return;
+    const int64_t step = (int64_t(gridDim.x) - first) * blockDim.x * 4;
+    // (dW is a float's multiple; whole pieces from the first 16-byte border on)
+    const int64_t head0 = (16 - (reinterpret_cast<uintptr_t>(dW) & 15)) / 4 & 3;
+    const int64_t head = head0 < count ? head0 : count;
+    const int64_t body = (count - head) / 4 * 4;
+    const int64_t at = ((int64_t(blockIdx.x) - first) * blockDim.x + threadIdx.x) * 4;
+    float4* p = reinterpret_cast<float4*>(dW + head);
+    for (int64_t i = at; i < body; i += step) p[i / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (int64_t(blockIdx.x) == first) {
+        if (threadIdx.x < head) dW[threadIdx.x] = 0.f;
+        if (head + body + threadIdx.x < count && threadIdx.x < 4) dW[head + body + threadIdx.x] = 0.f;
+    }
+}
+
+// The stable ranks of one digit among a workgroup's 1024 tokens.  A wavefront finds the
+// lanes that share a lane's digit bit by bit; its first of them counts for all.
+// counts [wavefronts, digits] must be zero; it is left with the tokens of each digit before
+// each wavefront's, and the digit's total in totals.
+__device__ __forceinline__ uint32_t rank_in_block(uint32_t digit, int bits, bool live,
+                                                  uint16_t (*counts)[kMaxDigits], uint32_t* totals)
+{
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    uint64_t same = __ballot(live);
+    for (int i = 0; i < bits; ++i) {
+        const uint64_t ones = __ballot(digit >> i & 1);
+        same &= digit >> i & 1 ? ones : ~ones;
+    }
+    const uint32_t before = __popcll(same & ((uint64_t(1) << lane) - 1));
+    if (live && before == 0) counts[wave][digit] = uint16_t(__popcll(same));
+    __syncthreads();
+    for (int d = threadIdx.x; d < 1 << bits; d += kSortBlock) {
+        uint32_t n = 0;
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t c = counts[w][d];
+            counts[w][d] = uint16_t(n);
+            n += c;
+        }
+        totals[d] = n;
+    }
+    __syncthreads();
+    return before + (live ? counts[wave][digit] : 0);
+}
+
+// Exclusive sums of up to kMaxDigits values, in place, by the first wavefront.
+__device__ __forceinline__ void exclusive_sum(uint32_t* v, int n)
+{
+    if (threadIdx.x < kWave) {
+        const int lane = threadIdx.x;
+        uint32_t base = 0;
+        for (int i = 0; i < n; i += kWave) {
+            const uint32_t x = i + lane < n ? v[i + lane] : 0;
+            uint32_t s = x;
+            for (int o = 1; o < kWave; o *= 2) {
+                const uint32_t y = __shfl_up(s, o, kWave);
+                if (lane >= o) s += y;
+            }
+            if (i + lane < n) v[i + lane] = base + s - x;
+            base += __shfl(s, kWave - 1, kWave);
+        }
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void clear_counts(uint16_t (*counts)[kMaxDigits])
+{
+    uint32_t* p = reinterpret_cast<uint32_t*>(counts);
+    for (int i = threadIdx.x; i < kSortWaves * kMaxDigits / 2; i += kSortBlock) p[i] = 0;
+    __syncthreads();
+}
+
+// All tokens in one workgroup; the others fill dW.
+__global__ __launch_bounds__(kSortBlock) void sort_small_kernel(
+    const int* __restrict__ ids, int n, uint32_t V, int passes, int bits, uint32_t* __restrict__ keys,
+    uint32_t* __restrict__ rows, float* dW, int64_t count)
+{
+    if (blockIdx.x > 0) {
+        fill_zeros(dW, count, 1);
+        return;
+    }
+    __shared__ uint32_t key[2][kSmall], row[2][kSmall];
+    __shared__ uint16_t counts[kSortWaves][kMaxDigits];
+    __shared__ uint32_t totals[kMaxDigits], first[kMaxDigits];
+    for (int i = threadIdx.x; i < n; i += kSortBlock) {
+        key[0][i] = key_of(ids[i], V);
+        row[0][i] = i;
+    }
+    __syncthreads();
+    const uint32_t mask = (1u << bits) - 1;
+    for (int p = 0; p < passes; ++p) {
+        const uint32_t *k = key[p & 1], *r = row[p & 1];
+        uint32_t *ko = key[~p & 1], *ro = row[~p & 1];
+        // where each digit's tokens begin: the totals of all rounds
+        for (int d = threadIdx.x; d <= int(mask); d += kSortBlock) first[d] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += kSortBlock) atomicAdd(&first[k[i] >> p * bits & mask], 1u);
+        __syncthreads();
+        exclusive_sum(first, int(mask) + 1);
+        for (int i0 = 0; i0 < n; i0 += kSortBlock) {
+            const int i = i0 + threadIdx.x;
+            const bool live = i < n;
+            clear_counts(counts);
+            const uint32_t x = live ? k[i] : 0, d = x >> p * bits & mask;
+            const uint32_t rank = rank_in_block(d, bits, live, counts, totals);
+            if (live) {
+                ko[first[d] + rank] = x;
+                ro[first[d] + rank] = r[i];
+            }
+            __syncthreads();
+            for (int j = threadIdx.x; j <= int(mask); j += kSortBlock) first[j] += totals[j];
+            __syncthreads();
+        }
+    }
+    for (int i = threadIdx.x; i < n; i += kSortBlock) {
+        keys[i] = key[passes & 1][i];
+        rows[i] = row[passes & 1][i];
+    }
+}
+
+// Tokens of each digit in each tile: counts [tiles, digits].  FIRST: the keys are the ids,
+// and the workgroups past the tiles fill dW.
+template <bool FIRST>
+__global__ __launch_bounds__(kSortBlock) void sort_count_kernel(
+    const uint32_t* __restrict__ keys, int64_t n, uint32_t V, int shift, int bits, int64_t tile,
+    int64_t tiles, uint32_t* __restrict__ counts, float* dW, int64_t count)
+{
+    if (FIRST && int64_t(blockIdx.x) >= tiles) {
+        fill_zeros(dW, count, tiles);
+        return;
+    }
+    __shared__ uint32_t total[kMaxDigits];
+    const uint32_t mask = (1u << bits) - 1;
+    for (int d = threadIdx.x; d <= int(mask); d += kSortBlock) total[d] = 0;
+    __syncthreads();
+    const int64_t i0 = blockIdx.x * tile, i1 = i0 + tile < n ? i0 + tile : n;
+    for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortBlock) {
+        const uint32_t k = FIRST ? key_of(int(keys[i]), V) : keys[i];
+        atomicAdd(&total[k >> shift & mask], 1u);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d <= int(mask); d += kSortBlock)
+        counts[blockIdx.x * int64_t(mask + 1) + d] = total[d];
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(kSortBlock) void sort_place_kernel(
+    const uint32_t* __restrict__ keys, const uint32_t* __restrict__ rows, int64_t n, uint32_t V,
+    int shift, int bits, int64_t tile, int64_t tiles, const uint32_t* __restrict__ counts,
+    uint32_t* __restrict__ keys_out, uint32_t* __restrict__ rows_out)
+{
+    __shared__ uint16_t in_wave[kSortWaves][kMaxDigits];
+    __shared__ uint32_t totals[kMaxDigits], first[kMaxDigits], mine[kMaxDigits];
+    const uint32_t mask = (1u << bits) - 1;
+    // a digit's first place in this tile: all tokens of lower digits, and its own in tiles before
+    for (int d = threadIdx.x; d <= int(mask); d += kSortBlock) {
+        uint32_t all = 0, before = 0;
+#pragma unroll 8
+        for (int64_t t = 0; t < tiles; ++t) {
+            const uint32_t c = counts[t * (mask + 1) + d];
+            before += t < int64_t(blockIdx.x) ? c : 0;
+            all += c;
+        }
+        first[d] = all;
+        mine[d] = before;
+    }
+    __syncthreads();
+    exclusive_sum(first, int(mask) + 1);
+    for (int d = threadIdx.x; d <= int(mask); d += kSortBlock) first[d] += mine[d];
+    const int64_t i1 = int64_t(blockIdx.x + 1) * tile < n ? int64_t(blockIdx.x + 1) * tile : n;
+    for (int64_t i0 = blockIdx.x * tile; i0 < i1; i0 += kSortBlock) {
+        const int64_t i = i0 + threadIdx.x;
+        const bool live = i < i1;
+        clear_counts(in_wave);
+        uint32_t x = live ? keys[i] : 0;
+        if (FIRST) x = key_of(int(x), V);
+        const uint32_t d = x >> shift & mask;
+        const uint32_t rank = rank_in_block(d, bits, live, in_wave, totals);
+        if (live) {
+            const uint32_t to = first[d] + rank;
+            keys_out[to] = x;
+            rows_out[to] = FIRST ? uint32_t(i) : rows[i];
+        }
+        __syncthreads();
+        for (int j = threadIdx.x; j <= int(mask); j += kSortBlock) first[j] += totals[j];
+        __syncthreads();
+    }
+}
+
+constexpr int kSumBlock = 256;
+
+// V sums to p, in pieces of 16 bytes.
+template <int V>
+__device__ __forceinline__ void put_sums(float* p, const float (&v)[V])
+{
+    if constexpr (V == 1) {
+        *p = v[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) {
+            const float x[4] = {v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+            put<4>(p + 4 * i, x);
+        }
+    }
+}
+
+// A window's tokens, run by run.  part [windows, 2, D]: the sum of the run that entered the
+// window (0) and of the one that leaves it and began in it (1).
+template <typename T, int V>
+__global__ __launch_bounds__(kSumBlock) void runs_kernel(
+    const T* __restrict__ dy, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ rows,
+    int64_t n, uint32_t rows_of_table, int64_t D, int window, float scale, bool accumulate,
+    float* __restrict__ dW, float* __restrict__ part)
+{
+    const int64_t blocks = (D + kSumBlock * V - 1) / (kSumBlock * V);
+    const int64_t w = blockIdx.x / blocks;
+    const int64_t c0 = (blockIdx.x % blocks * kSumBlock + threadIdx.x) * V;
+    if (c0 >= D) return;
+    // (a piece that would pass the row's end starts before it: two lanes store the same bits,
+    // but where they add to what is there, which only the one that owns a value may)
+    const int64_t c = c0 + V <= D ? c0 : D - V;
+    const int twice = int(c0 - c);
+    const int64_t p0 = w * window, p1 = p0 + window < n ? p0 + window : n;
+    const uint32_t entered = p0 > 0 ? keys[p0 - 1] : ~0u, leaves = p1 < n ? keys[p1] : ~0u;
+    if (keys[p0] >= rows_of_table) return;
+    bool in_run = keys[p0] == entered;  // of a token before the window
+    float acc[V] = {};
+    auto close = [&](int64_t p, uint32_t key) {  // the run that ends with token p
+        if (p + 1 == p1 && key == leaves) {
+            put_sums<V>(part + (w * 2 + (in_run ? 0 : 1)) * D + c, acc);
+        } else if (in_run) {
+            put_sums<V>(part + w * 2 * D + c, acc);
+        } else {
+            float* out = dW + int64_t(key) * D + c;
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] *= scale;
+            if (accumulate) {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (j >= twice) out[j] += acc[j];
+            } else {
+                put_sums<V>(out, acc);
+            }
+        }
+        in_run = false;
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = 0.f;
+    };
+    constexpr int kAhead = 8;
+    for (int64_t p = p0; p < p1; p += kAhead) {
+        Raw<T, V> raw[kAhead];
+        uint32_t key[kAhead + 1];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t q = p + i < p1 ? p + i : p1 - 1;
+            key[i] = keys[q];
+            raw[i] = load_raw<V>(dy + int64_t(rows[q]) * D + c);
+        }
+        key[kAhead] = p + kAhead < p1 ? keys[p + kAhead] : ~0u;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (p + i >= p1 || key[i] >= rows_of_table) break;
+            float v[V];
+            expand<V, T>(raw[i], v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] += v[j];
+            if (p + i + 1 == p1 || key[i + 1] != key[i]) close(p + i, key[i]);
+        }
+    }
+}
+
+// Runs that cross windows, each by the workgroups of the window that it begins in.
+__global__ __launch_bounds__(kSumBlock) void joins_kernel(
+    const uint32_t* __restrict__ keys, int64_t n, uint32_t rows_of_table, int64_t D, int window,
+    float scale, bool accumulate, float* __restrict__ dW, const float* __restrict__ part)
+{
+    const int64_t blocks = (D + kSumBlock - 1) / kSumBlock;
+    const int64_t w = blockIdx.x / blocks;
+    const int64_t c = blockIdx.x % blocks * kSumBlock + threadIdx.x;
+    const int64_t p0 = w * window, p1 = p0 + window;
+    if (p1 >= n) return;
+    const uint32_t key = keys[p1 - 1];
+    if (key >= rows_of_table || keys[p1] != key) return;          // nothing leaves
+    if (keys[p0] == key && p0 > 0 && keys[p0 - 1] == key) return;  // it began before
+    if (c >= D) return;
+    // the last window that the run reaches: its first token is of the run
+    const int64_t windows = (n + window - 1) / window;
+    int64_t last = w + 1, hi = windows - 1;
+    while (last < hi) {
+        const int64_t mid = (last + hi + 1) / 2;
+        if (keys[mid * window] == key) last = mid;
+        else hi = mid - 1;
+    }
+    float acc = part[(w * 2 + 1) * D + c];
+    int64_t j = w + 1;
+    for (; j + 7 <= last; j += 8) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = part[(j + i) * 2 * D + c];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc += v[i];
+    }
+    for (; j <= last; ++j) acc += part[j * 2 * D + c];
+    float* out = dW + int64_t(key) * D + c;
+    *out = accumulate ? *out + acc * scale : acc * scale;
+}
+
+size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
+
+template <typename T>
+hipError_t launch_runs(const T* dy, const uint32_t* keys, const uint32_t* rows, int64_t n, int64_t V,
+                       int64_t D, const EmbedGradPlan& p, float scale, bool accumulate, float* dW,
+                       float* part, hipStream_t stream)
+{
+    constexpr int kV = kVec<T>;
+    const int v = D < kV ? 1 : kV;
+    const dim3 grid(uint32_t(p.windows * ((D + kSumBlock * v - 1) / (kSumBlock * v))));
+    if (v == 1)
+        hipLaunchKernelGGL((runs_kernel<T, 1>), grid, dim3(kSumBlock), 0, stream, dy, keys, rows, n,
+                           uint32_t(V), D, int(p.window), scale, accumulate, dW, part);
+    else
+        hipLaunchKernelGGL((runs_kernel<T, kV>), grid, dim3(kSumBlock), 0, stream, dy, keys, rows, n,
+                           uint32_t(V), D, int(p.window), scale, accumulate, dW, part);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+EmbedGradPlan embed_grad_plan(int64_t n, int64_t V, int64_t D)
+{
+    EmbedGradPlan p{};
+    p.window = n <= 8192 ? 16 : 64;
+    p.windows = (n + p.window - 1) / p.window;
+    int bits = 1;  // of the keys 0 .. V
+    while (V >> bits) ++bits;
+    p.passes = (bits + kMaxBits - 1) / kMaxBits;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    if (n > kSmall) {
+        // at most 128 tiles, over whose counts every tile sums
+        p.tile = ((n + 127) / 128 + kSortBlock - 1) / kSortBlock * kSortBlock;
+        p.tiles = (n + p.tile - 1) / p.tile;
+    }
+    size_t at = 0;
+    for (int i = 0; i < 2; ++i) {
+        p.off_keys[i] = at, at += aligned(4 * size_t(n));
+        p.off_rows[i] = at, at += aligned(4 * size_t(n));
+    }
+    p.off_counts = at, at += aligned(4 * size_t(p.tiles) << p.bits);
+    p.off_part = at, at += 8 * size_t(p.windows) * D;
+    p.ws_bytes = n > 0 ? at : 0;
+    return p;
+}
+
+int64_t embed_grad_threads(int64_t n, int64_t V, int64_t D)
+{
+    const EmbedGradPlan p = embed_grad_plan(n, V, D);
+    const int64_t sum = p.windows * ((D + kSumBlock - 1) / kSumBlock) * kSumBlock;
+    const int64_t sort = (p.tiles + 1 + kFillBlocks) * kSortBlock;
+    return sum > sort ? sum : sort;
+}
+
+hipError_t launch_embed_grad(const void* dy, const int32_t* ids, int64_t n, int64_t V, int64_t D,
+                             bool bf16_io, float scale, bool accumulate, float* dW, void* workspace,
+                             hipStream_t stream)
+{
+    const EmbedGradPlan p = embed_grad_plan(n, V, D);
+    char* ws = static_cast<char*>(workspace);
+    uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + p.off_keys[0]), reinterpret_cast<uint32_t*>(ws + p.off_keys[1])};
+    uint32_t* rows[2] = {reinterpret_cast<uint32_t*>(ws + p.off_rows[0]), reinterpret_cast<uint32_t*>(ws + p.off_rows[1])};
+    float* part = reinterpret_cast<float*>(ws + p.off_part);
+    float* fill = accumulate ? nullptr : dW;
+    const int64_t count = V * D;
+    // workgroups that fill: 16 KiB each at least
+    int64_t fills = fill ? (count + 4095) / 4096 : 0;
+    fills = fills < kFillBlocks ? fills : kFillBlocks;
+    hipError_t e;
+    int at = 0;  // where the sorted tokens are
+    if (p.tiles == 0) {
+        if (n == 0 && fills == 0) return hipSuccess;
+        hipLaunchKernelGGL(sort_small_kernel, dim3(uint32_t(1 + fills)), dim3(kSortBlock), 0, stream, ids,
+                           int(n), uint32_t(V), p.passes, p.bits, keys[0], rows[0], fill, count);
+        if ((e = hipGetLastError()) != hipSuccess || n == 0) return e;
+    } else {
+        uint32_t* counts = reinterpret_cast<uint32_t*>(ws + p.off_counts);
+        const dim3 grid(uint32_t(p.tiles)), block(kSortBlock);
+        for (int i = 0; i < p.passes; ++i) {
+            const int shift = i * p.bits;
+            if (i == 0) {
+                const uint32_t* in = reinterpret_cast<const uint32_t*>(ids);
+                hipLaunchKernelGGL((sort_count_kernel<true>), dim3(uint32_t(p.tiles + fills)), block, 0, stream,
+                                   in, n, uint32_t(V), shift, p.bits, p.tile, p.tiles, counts, fill, count);
+                if ((e = hipGetLastError()) != hipSuccess) return e;
+                hipLaunchKernelGGL((sort_place_kernel<true>), grid, block, 0, stream, in,
+                                   static_cast<const uint32_t*>(nullptr), n, uint32_t(V), shift, p.bits, p.tile,
+                                   p.tiles, counts, keys[0], rows[0]);
+            } else {
+                hipLaunchKernelGGL((sort_count_kernel<false>), grid, block, 0, stream, keys[at], n, uint32_t(V),
+                                   shift, p.bits, p.tile, p.tiles, counts, static_cast<float*>(nullptr), int64_t(0));
+                if ((e = hipGetLastError()) != hipSuccess) return e;
+                hipLaunchKernelGGL((sort_place_kernel<false>), grid, block, 0, stream, keys[at], rows[at], n,
+                                   uint32_t(V), shift, p.bits, p.tile, p.tiles, counts, keys[at ^ 1], rows[at ^ 1]);
+                at ^= 1;
+            }
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+    }
+    e = bf16_io ? launch_runs(static_cast<const bf16*>(dy), keys[at], rows[at], n, V, D, p, scale, accumulate,
+                              dW, part, stream)
+                : launch_runs(static_cast<const float*>(dy), keys[at], rows[at], n, V, D, p, scale, accumulate,
+                              dW, part, stream);
+    if (e != hipSuccess) return e;
+    const int64_t blocks = (D + kSumBlock - 1) / kSumBlock;
+    hipLaunchKernelGGL(joins_kernel, dim3(uint32_t(p.windows * blocks)), dim3(kSumBlock), 0, stream, keys[at], n,
+                       uint32_t(V), D, int(p.window), scale, accumulate, dW, part);
+    return hipGetLastError();
+}
+
+}  // namespace lh
