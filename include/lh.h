@@ -626,7 +626,7 @@ lh_status lh_selective_backward(const lh_selective_inputs* in, const lh_selectiv
  */
 
 /* The gated recurrence keeps the state before every LH_GATED_MARK-th token for its gradient. */
-#define LH_GATED_MARK 64
+#define LH_GATED_MARK 8
 
 /*
  * Gated linear recurrence.  Per batch row and channel c:
@@ -665,6 +665,7 @@ size_t lh_gated_workspace_bytes(int64_t B, int64_t T, int64_t D);
  *               where a row has no such token; NULL where not needed
  *   workspace : lh_gated_workspace_bytes bytes, 256-byte aligned (NULL allowed when that
  *               is 0)
+ * Every ld must be less than 2^26 here and in the gradient (not in a step).
  * One kernel launch, or two where the prompt is cut into chunks.
  */
 lh_status lh_gated_prefill(const lh_gated_inputs* in, int resume, float* state, void* y,

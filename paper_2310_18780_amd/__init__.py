@@ -102,7 +102,7 @@ PLAN_MFMA_SEG = -2
 # scratch that lh_prefill_noalloc holds per GPU
 NOALLOC_SCRATCH_BYTES = 64 << 20
 # tokens between the states that gated_prefill leaves for gated_backward
-GATED_MARK = 64
+GATED_MARK = 8
 STATUS = {
     0: "LH_OK",
     1: "LH_ERR_INVALID_ARG",

@@ -4,15 +4,18 @@
 //   h <- a h + sqrt(1 - a^2) p u,   y = h (times z sigmoid(z))
 //
 // h after any run of steps is A h_before + H, with A the product of the run's decays and
-// H what its inputs alone leave.  A workgroup of 16 wavefronts holds 64 channels of a row,
-// one to a lane, and walks the time in blocks of 128 steps, 8 to a wavefront: each
-// wavefront forms (A, H) of its run, they meet in LDS, each chains those before its own to
-// its entry state and walks its steps again from registers.  Inputs are read once, outputs
-// written once.  Where rows are few the prompt is cut into chunks; a first launch forms
-// each chunk's (log2 A, H), and each chunk of the second folds those before it.
+// H what its inputs alone leave.  A wavefront holds 64 channels of a row, one to a lane, and
+// takes 8 steps at a time, whose loads all start together.
 //
-// A block's decay is carried on as the sum of its logarithms (carry_on): products of
-// roundings near 1 would be off by 2^-24 a step over thousands of steps.
+// Many rows: a workgroup of 16 wavefronts walks a prompt in blocks of 128 steps, 8 to a
+// wavefront.  Each forms (A, H) of its run, they meet in LDS, each chains those before its own
+// to its entry state and walks its steps again from registers: inputs are read once, outputs
+// written once.  Few rows: the prompt is cut into chunks, one to a wavefront that walks it by
+// itself; a first launch forms each chunk's (log2 A, H), and each chunk of the second folds those
+// before it.
+//
+// A run's decay is carried on as the sum of its logarithms (carry_on): products of roundings
+// near 1 would be off by 2^-24 a step over thousands of steps.
 #include "gated_ops.hpp"
 
 namespace lh {
@@ -20,123 +23,147 @@ namespace {
 
 constexpr int kWaves = 16;
 constexpr int kSpan = kWaves * kRun;  // steps of a block
-static_assert(kSpan % kMark == 0, "marks lie before runs");
 
-// ENDS: the chunks' ends only, into slots 1 .. of ends [B, chunks, D] (log2 of the decay,
-// negated, and state from zero); slot 0 holds the start.
-template <typename T, bool GATE, bool ENDS>
-__global__ __launch_bounds__(kWaves* kWave) void gated_kernel(
-    GatedIn<T> in, float* state, int resume, T* __restrict__ y, float* __restrict__ marks,
-    float2* __restrict__ ends)
+// The inputs of a run, as they lie in memory.
+template <typename T, bool GATE>
+struct Run {
+    T r[kRun], i[kRun], u[kRun], z[kRun];
+    __device__ __forceinline__ Run(const GatedIn<T>& in, const Place& at, int64_t t, int m)
+    {
+        const int64_t row = at.b * in.T_ + t;
+        const uint32_t lane = at.lc * uint32_t(sizeof(T));
+        const Rows<T> br(in.r + row * in.ld_r + at.c0, in.ld_r, at.wide, m);
+        const Rows<T> bi(in.i + row * in.ld_i + at.c0, in.ld_i, at.wide, m);
+        const Rows<T> bu(in.u + row * in.ld_u + at.c0, in.ld_u, at.wide, m);
+#pragma unroll
+        for (int s = 0; s < kRun; ++s) {
+            r[s] = br.load(s, lane);
+            i[s] = bi.load(s, lane);
+            u[s] = bu.load(s, lane);
+        }
+        if constexpr (GATE) {
+            const Rows<T> bz(in.z + row * in.ld_z + at.c0, in.ld_z, at.wide, m);
+#pragma unroll
+            for (int s = 0; s < kRun; ++s) z[s] = bz.load(s, lane);
+        }
+    }
+    // step s of m: steps past the last decay nothing, and their inputs are zeros
+    __device__ __forceinline__ GateStep step(int s, int m, const GateParams& par) const
+    {
+        return gate_step(io_load(&r[s]), io_load(&i[s]), io_load(&u[s]), s < m, par);
+    }
+    __device__ __forceinline__ float out(int s, float h) const
+    {
+        if constexpr (!GATE) return h;
+        const float g = io_load(&z[s]);
+        return h * (g * sigmoid(g));
+    }
+};
+
+template <typename T, bool GATE>
+__global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, float* state, int resume,
+                                                              T* __restrict__ y, float* __restrict__ marks)
 {
     __shared__ float2 runs[2][kWaves][kWave];
     __shared__ float logs[2][kWaves][kWave];
     const int lane = threadIdx.x % kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t tile = blockIdx.x % in.tiles;
-    const int64_t per = ENDS ? in.chunks - 1 : in.chunks;
-    const int64_t k = blockIdx.x / in.tiles % per;
-    const int64_t b = blockIdx.x / in.tiles / per;
-    // Lanes past the last channel repeat it: they store the same bits to the same place.
-    const int64_t c0 = tile * kTile;
-    const uint32_t lc = uint32_t(c0 + lane < in.D ? lane : in.D - 1 - c0);
-    const int64_t c = c0 + lc;
+    const Place at(in, blockIdx.x, 1, 0);
+    const int64_t c = at.c0 + at.lc;
     const GateParams par(in, c);
-    const int64_t n = gated_length(in.lengths, b, in.T_);
-    const int64_t t0 = k * in.chunk;
-    const int64_t t1 = t0 + in.chunk < in.T_ ? t0 + in.chunk : in.T_;
-    const int64_t te = t1 < n ? t1 : n;  // the chunk's tokens end here
-
-    float h = 0.f, total = 0.f;  // state before the block; log2 of the decays so far, negated
-    if constexpr (ENDS) {
-        if (k == 0 && wave == 0)
-            ends[b * in.chunks * in.D + c] = make_float2(0.f, resume ? state[b * in.D + c] : 0.f);
-    } else if (in.chunks == 1) {
-        if (resume) h = state[b * in.D + c];
-    } else {
-        const float2* e = ends + b * in.chunks * in.D + c;
-        for (int64_t j = 0; j <= k; ++j) {
-            const float2 v = e[j * in.D];
-            h = carry_on(h, v.x, v.y);
-        }
-    }
-
-    // (a uniform row's address and a lane's offset)
-    const T* pr = in.r + b * in.T_ * in.ld_r + c0;
-    const T* pi = in.i + b * in.T_ * in.ld_i + c0;
-    const T* pu = in.u + b * in.T_ * in.ld_u + c0;
-    const T* pz = GATE && !ENDS ? in.z + b * in.T_ * in.ld_z + c0 : nullptr;
-    T* py = ENDS ? nullptr : y + b * in.T_ * in.D + c0;
-
-    T r[kRun], i[kRun], u[kRun], z[kRun];
-    // a step past the tokens reads the last one again and takes no part
-    auto load = [&](int64_t t) {
-#pragma unroll
-        for (int s = 0; s < kRun; ++s) {
-            const int64_t row = t + s < te ? t + s : te - 1;
-            r[s] = (pr + row * in.ld_r)[lc];
-            i[s] = (pi + row * in.ld_i)[lc];
-            u[s] = (pu + row * in.ld_u)[lc];
-            if constexpr (GATE && !ENDS) z[s] = (pz + row * in.ld_z)[lc];
-        }
-    };
+    float h = resume ? state[at.b * in.D + c] : 0.f;  // before the block
     int turn = 0;
-    if (t0 < te) load(t0 + wave * kRun);
-    for (int64_t tb = t0; tb < te; tb += kSpan, turn ^= 1) {
+    for (int64_t tb = 0; tb < at.te; tb += kSpan, turn ^= 1) {
         const int64_t t = tb + wave * kRun;
-        const int m = int(te - t < kRun ? te - t : kRun);  // steps of this run (<= 0: none)
-        float a[kRun], v[kRun], gate[kRun];
+        const int m = int(at.te - t < kRun ? at.te - t : kRun);  // steps (<= 0: none)
+        const Run<T, GATE> x(in, at, t, m);
+        float a[kRun], v[kRun];
         float H = 0.f, L = 0.f;
 #pragma unroll
         for (int s = 0; s < kRun; ++s) {
-            const float f = rcp_fast(1.f + exp2_fast(fmaf(io_load(&r[s]), -kLog2e, par.nrb)));
-            const float p = rcp_fast(1.f + exp2_fast(fmaf(io_load(&i[s]), -kLog2e, par.nib)));
-            const float l = par.rate2 * f;
-            const float as = exp2_fast(-l);
-            const float q = one_minus(2.f * l, as * as);
-            const float vs = __builtin_amdgcn_sqrtf(q) * p * io_load(&u[s]);
-            a[s] = s < m ? as : 1.f;
-            v[s] = s < m ? vs : 0.f;
-            L += s < m ? l : 0.f;
+            const GateStep g = x.step(s, m, par);
+            a[s] = g.a;
+            v[s] = g.v;
+            L += g.l;
             H = fmaf(a[s], H, v[s]);
-            if constexpr (GATE && !ENDS) {
-                const float zs = io_load(&z[s]);
-                gate[s] = zs * sigmoid(zs);
-            }
         }
-        if (tb + kSpan < te) load(t + kSpan);
         runs[turn][wave][lane] = make_float2(exp2_fast(-L), H);
         logs[turn][wave][lane] = L;
         __syncthreads();
         // from zero: the states and decays before this run, and of the whole block
         float e = 0.f, le = 0.f, end = 0.f, lend = 0.f;
-#pragma unroll
+#pragma unroll 4
         for (int j = 0; j < kWaves; ++j) {
             if (j == wave) e = end, le = lend;
-            const float2 x = runs[turn][j][lane];
-            end = fmaf(x.x, end, x.y);
+            const float2 n = runs[turn][j][lane];
+            end = fmaf(n.x, end, n.y);
             lend += logs[turn][j][lane];
         }
-        if constexpr (!ENDS) {
-            float x = fmaf(exp2_fast(-le), h, e);
-            if (wave == 0) x = h;
-            if (marks && t % kMark == 0 && t < te)
-                marks[(b * in.marks + t / kMark) * in.D + c] = x;
+        float o = wave == 0 ? h : fmaf(exp2_fast(-le), h, e);
+        if (marks && m > 0) marks[(at.b * in.marks + t / kRun) * in.D + c] = o;
+        const Rows<T> by(y + (at.b * in.T_ + t) * in.D + at.c0, in.D, at.wide, m);
 #pragma unroll
-            for (int s = 0; s < kRun; ++s) {
-                x = fmaf(a[s], x, v[s]);
-                if (s < m) io_store(py + (t + s) * in.D + lc, GATE ? x * gate[s] : x);
-            }
+        for (int s = 0; s < kRun; ++s) {
+            o = fmaf(a[s], o, v[s]);
+            by.store(s, at.lc * uint32_t(sizeof(T)), x.out(s, o));
         }
         h = carry_on(h, lend, end);
-        total += lend;
+    }
+    for (int64_t t = at.te + wave; t < in.T_; t += kWaves) io_store(y + (at.b * in.T_ + t) * in.D + c, 0.f);
+    if (wave == 0) state[at.b * in.D + c] = h;
+}
+
+constexpr int kWalkWaves = 4;  // wavefronts of a workgroup, each with a chunk of its own
+
+// ENDS: the chunks' ends only, into slots 1 .. of ends [B, chunks, D] (log2 of the decay,
+// negated, and state from zero); slot 0 holds the start.
+template <typename T, bool GATE, bool ENDS>
+__global__ __launch_bounds__(kWalkWaves* kWave) void gated_walk_kernel(
+    GatedIn<T> in, float* state, int resume, T* __restrict__ y, float* __restrict__ marks,
+    float2* __restrict__ ends, int64_t units)
+{
+    const int64_t unit = int64_t(blockIdx.x) * kWalkWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    if (unit >= units) return;
+    const Place at(in, unit, ENDS ? in.chunks - 1 : in.chunks, 0);
+    const int64_t c = at.c0 + at.lc;
+    const GateParams par(in, c);
+    float h = 0.f, total = 0.f;  // state; log2 of the decays so far, negated
+    float2* pe = ends + at.b * in.chunks * in.D + c;
+    if constexpr (ENDS) {
+        if (at.k == 0) pe[0] = make_float2(0.f, resume ? state[at.b * in.D + c] : 0.f);
+    } else if (in.chunks == 1) {
+        if (resume) h = state[at.b * in.D + c];
+    } else if (at.t0 < at.te || at.k == in.chunks - 1) {
+        for (int64_t j = 0; j <= at.k; ++j) {
+            const float2 v = pe[j * in.D];
+            h = carry_on(h, v.x, v.y);
+        }
+    }
+    for (int64_t t = at.t0; t < at.te; t += kRun) {
+        const int m = int(at.te - t < kRun ? at.te - t : kRun);
+        const Run<T, GATE && !ENDS> x(in, at, t, m);
+        if (!ENDS && marks) marks[(at.b * in.marks + t / kRun) * in.D + c] = h;
+        float H = 0.f, L = 0.f, o = h;
+        const Rows<T> by(y + (at.b * in.T_ + t) * in.D + at.c0, in.D, at.wide, m);
+#pragma unroll
+        for (int s = 0; s < kRun; ++s) {
+            const GateStep g = x.step(s, m, par);
+            L += g.l;
+            H = fmaf(g.a, H, g.v);
+            if constexpr (!ENDS) {
+                o = fmaf(g.a, o, g.v);
+                by.store(s, at.lc * uint32_t(sizeof(T)), x.out(s, o));
+            }
+        }
+        h = carry_on(h, L, H);
+        total += L;
     }
     if constexpr (ENDS) {
-        if (wave == 0) ends[(b * in.chunks + k + 1) * in.D + c] = make_float2(total, h);
+        pe[(at.k + 1) * in.D] = make_float2(total, h);
     } else {
-        for (int64_t t = (te > t0 ? te : t0) + wave; t < t1; t += kWaves)
-            io_store(py + t * in.D + lc, 0.f);
-        if (k == in.chunks - 1 && wave == 0) state[b * in.D + c] = h;
+        for (int64_t t = at.te > at.t0 ? at.te : at.t0; t < at.t1; ++t)
+            io_store(y + (at.b * in.T_ + t) * in.D + c, 0.f);
+        if (at.k == in.chunks - 1) state[at.b * in.D + c] = h;
     }
 }
 
@@ -150,12 +177,9 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedIn<T> in, float* _
     const int64_t b = blockIdx.x / blocks;
     if (c >= in.D) return;
     const GateParams par(in, c);
-    const float r = io_load(in.r + b * in.ld_r + c), i = io_load(in.i + b * in.ld_i + c);
-    const float u = io_load(in.u + b * in.ld_u + c), h = state[b * in.D + c];
-    const float f = rcp_fast(1.f + exp2_fast(fmaf(r, -kLog2e, par.nrb)));
-    const float p = rcp_fast(1.f + exp2_fast(fmaf(i, -kLog2e, par.nib)));
-    const float l = par.rate2 * f, a = exp2_fast(-l);
-    const float x = carry_on(h, l, __builtin_amdgcn_sqrtf(one_minus(2.f * l, a * a)) * p * u);
+    const GateStep g = gate_step(io_load(in.r + b * in.ld_r + c), io_load(in.i + b * in.ld_i + c),
+                                 io_load(in.u + b * in.ld_u + c), true, par);
+    const float x = carry_on(state[b * in.D + c], g.l, g.v);
     state[b * in.D + c] = x;
     float o = x;
     if (in.z) {
@@ -165,26 +189,32 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedIn<T> in, float* _
     io_store(y + b * in.D + c, o);
 }
 
-template <typename T>
+// Workgroups of 16 wavefronts from here on (half again as many as CUs).
+constexpr int64_t kManyTiles = 384;
+
+template <typename T, bool GATE>
 hipError_t gated(const Gated& g, float* state, bool resume, T* y, float* marks, float2* ends,
                  hipStream_t stream)
 {
     const GatedPlan p = gated_plan(g.B, g.T, g.D);
     const GatedIn<T> in = gated_in<T>(g, p);
-    const dim3 block(kWaves * kWave);
+    const int64_t tiles = gated_tiles(g.B, g.D);
+    if (tiles >= kManyTiles) {
+        hipLaunchKernelGGL((gated_kernel<T, GATE>), dim3(uint32_t(tiles)), dim3(kWaves * kWave), 0, stream, in,
+                           state, int(resume), y, marks);
+        return hipGetLastError();
+    }
+    const dim3 block(kWalkWaves * kWave);
+    auto grid = [](int64_t units) { return dim3(uint32_t((units + kWalkWaves - 1) / kWalkWaves)); };
     if (p.chunks > 1) {
-        hipLaunchKernelGGL((gated_kernel<T, false, true>), dim3(uint32_t(g.B * in.tiles * (p.chunks - 1))),
-                           block, 0, stream, in, state, int(resume), static_cast<T*>(nullptr),
-                           static_cast<float*>(nullptr), ends);
+        const int64_t units = tiles * (p.chunks - 1);
+        hipLaunchKernelGGL((gated_walk_kernel<T, GATE, true>), grid(units), block, 0, stream, in, state,
+                           int(resume), static_cast<T*>(nullptr), static_cast<float*>(nullptr), ends, units);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    const dim3 grid(uint32_t(g.B * in.tiles * p.chunks));
-    if (g.z)
-        hipLaunchKernelGGL((gated_kernel<T, true, false>), grid, block, 0, stream, in, state, int(resume),
-                           y, marks, ends);
-    else
-        hipLaunchKernelGGL((gated_kernel<T, false, false>), grid, block, 0, stream, in, state, int(resume),
-                           y, marks, ends);
+    const int64_t units = tiles * p.chunks;
+    hipLaunchKernelGGL((gated_walk_kernel<T, GATE, false>), grid(units), block, 0, stream, in, state, int(resume),
+                       y, marks, ends, units);
     return hipGetLastError();
 }
 
@@ -192,22 +222,17 @@ hipError_t gated(const Gated& g, float* state, bool resume, T* y, float* marks, 
 
 GatedPlan gated_plan(int64_t B, int64_t T, int64_t D)
 {
-    // two workgroups to a CU
-    const int64_t tiles = gated_tiles(B, D), spans = (T + kSpan - 1) / kSpan;
-    int64_t chunks = tiles >= 384 ? 1 : (512 + tiles - 1) / tiles;
-    if (chunks > spans) chunks = spans;
-    if (chunks < 1) chunks = 1;
-    const int64_t per = spans > 0 ? (spans + chunks - 1) / chunks : 1;
-    GatedPlan p;
-    p.chunk = per * kSpan;
-    p.chunks = spans > 0 ? (spans + per - 1) / per : 1;
+    const int64_t tiles = gated_tiles(B, D);
+    if (tiles >= kManyTiles) return GatedPlan{T > 0 ? T : 1, 1, 0};
+    GatedPlan p = gated_chunks(B, T, D, 4096, 64);
     p.ws_bytes = p.chunks > 1 ? sizeof(float2) * size_t(B) * p.chunks * D : 0;
     return p;
 }
 
 int64_t gated_threads(int64_t B, int64_t T, int64_t D)
 {
-    return gated_tiles(B, D) * gated_plan(B, T, D).chunks * kWaves * kWave;
+    const int64_t tiles = gated_tiles(B, D);
+    return tiles >= kManyTiles ? tiles * kWaves * kWave : (tiles * gated_plan(B, T, D).chunks + kWalkWaves) * kWave;
 }
 
 int64_t gated_step_threads(int64_t B, int64_t D) { return B * ((D + 255) / 256) * 256; }
@@ -216,8 +241,11 @@ hipError_t launch_gated(const Gated& g, float* state, bool resume, void* y, floa
                         void* workspace, hipStream_t stream)
 {
     float2* ends = static_cast<float2*>(workspace);
-    if (g.bf16_io) return gated(g, state, resume, static_cast<bf16*>(y), marks, ends, stream);
-    return gated(g, state, resume, static_cast<float*>(y), marks, ends, stream);
+    if (g.bf16_io)
+        return g.z ? gated<bf16, true>(g, state, resume, static_cast<bf16*>(y), marks, ends, stream)
+                   : gated<bf16, false>(g, state, resume, static_cast<bf16*>(y), marks, ends, stream);
+    return g.z ? gated<float, true>(g, state, resume, static_cast<float*>(y), marks, ends, stream)
+               : gated<float, false>(g, state, resume, static_cast<float*>(y), marks, ends, stream);
 }
 
 hipError_t launch_gated_step(const Gated& g, float* state, void* y_t, hipStream_t stream)

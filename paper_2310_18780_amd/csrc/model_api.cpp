@@ -45,6 +45,11 @@ lh_status check_gated(const lh_gated_inputs* in, Form form)
     if ((s = check_ld("ld_r", in->ld_r, in->D, rows)) || (s = check_ld("ld_i", in->ld_i, in->D, rows)) ||
         (s = check_ld("ld_u", in->ld_u, in->D, rows)) || (in->z && (s = check_ld("ld_z", in->ld_z, in->D, rows))))
         return s;
+    // (a run's rows are addressed in 32 bits)
+    if (form == Form::kStep) return LH_OK;
+    for (const int64_t ld : {in->ld_r, in->ld_i, in->ld_u, in->z ? in->ld_z : 0})
+        if (ld >= (INT64_C(1) << 26))
+            return fail(LH_ERR_INVALID_ARG, "rows must be less than 2^26 elements apart, got %lld", (long long)ld);
     return LH_OK;
 }
 

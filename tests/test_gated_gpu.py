@@ -205,7 +205,7 @@ def test_gradients_against_differences():
     B, T, D = 2, 90, 33
     c = case(B, T, D, "f32", seed=20)
     dy = dev(gen(21).normal(size=(B, T, D)))
-    marks = nan_like((B, 2, D))
+    marks = nan_like((B, -(-T // lh.GATED_MARK), D))
 
     def value(c):
         y = nan_like((B, T, D))
@@ -236,7 +236,7 @@ def test_rates_at_their_ends():
     c["r"][0, 5] = float("inf")
     c["i"][0, 7], c["i"][0, 9] = float("-inf"), float("inf")
     start = dev(np.ones((B, D)))
-    y, state, marks = nan_like((B, T, D)), start.clone(), nan_like((B, 3, D))
+    y, state, marks = nan_like((B, T, D)), start.clone(), nan_like((B, -(-T // lh.GATED_MARK), D))
     lh.gated_prefill(state=state, y=y, resume=True, marks=marks, **c)
     args = ref_args(c)
     args["rate"] = np.minimum(args["rate"], 2e38)
@@ -297,15 +297,16 @@ def test_offsets_past_32_bits():
     g = torch.Generator(device="cuda").manual_seed(1)
     u = torch.empty((1, T, D), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
     rate, bias = dev(np.exp(gen(2).uniform(-2, 1, D))), dev(gen(3).normal(size=D))
-    y, marks, s = torch.empty_like(u), torch.empty((1, -(-T // 64), D), device="cuda"), nan_like((1, D))
+    M = lh.GATED_MARK
+    y, marks, s = torch.empty_like(u), torch.empty((1, -(-T // M), D), device="cuda"), nan_like((1, D))
     lh.gated_prefill(rate, u, u, u, s, y, r_bias=bias, marks=marks)
-    k = (T - tail) // 64  # a mark
-    n = T - 64 * k
-    state, part, m2 = marks[:, k].clone(), torch.empty((1, n, D), dtype=torch.bfloat16, device="cuda"), nan_like((1, -(-n // 64), D))
-    x = u[:, 64 * k:].contiguous()
+    k = (T - tail) // M  # a mark
+    n = T - M * k
+    state, part, m2 = marks[:, k].clone(), torch.empty((1, n, D), dtype=torch.bfloat16, device="cuda"), nan_like((1, -(-n // M), D))
+    x = u[:, M * k:].contiguous()
     lh.gated_prefill(rate, x, x, x, state, part, r_bias=bias, resume=True, marks=m2)
     # the same tokens from the same state, cut elsewhere: 2^-8 of the outputs' rounding, and of their scale
-    assert (part.float() - y[:, 64 * k:].float()).abs().max().item() <= 2.0 ** -7 * part.float().abs().max().item()
+    assert (part.float() - y[:, M * k:].float()).abs().max().item() <= 2.0 ** -7 * part.float().abs().max().item()
     assert (state - s).abs().max().item() <= 1e-4 * s.abs().max().item()
     # gradients that only the last tokens get
     dy = torch.zeros_like(u)
@@ -314,7 +315,7 @@ def test_offsets_past_32_bits():
     dr = [nan_like((D,)) for _ in range(2)]
     lh.gated_backward(dy, rate, u, u, u, marks, dr[0], *big, r_bias=bias)
     small = [torch.empty_like(x) for _ in range(3)]
-    lh.gated_backward(dy[:, 64 * k:].contiguous(), rate, x, x, x, m2, dr[1], *small, r_bias=bias)
+    lh.gated_backward(dy[:, M * k:].contiguous(), rate, x, x, x, m2, dr[1], *small, r_bias=bias)
     for a, b in zip(big, small):
-        a = a[:, 64 * k:]
+        a = a[:, M * k:]
         assert (a.float() - b.float()).abs().max().item() <= 2.0 ** -6 * b.float().abs().max().item()

@@ -51,6 +51,7 @@ def test_gated_refusals():
     refused(INVALID, gated(y=None), "NULL")
     refused(INVALID, gated(ld_i=7), "ld_i")
     refused(INVALID, gated(ld_z=7), "ld_z")
+    refused(INVALID, gated(ld_u=1 << 26), "2^26")
     refused(INVALID, gated(r=A + 3 * MB + 2), "aligned")
     refused(INVALID, gated(lengths=A + 10 * MB + 1), "aligned")
     refused(DTYPE, gated(io_dtype=2))

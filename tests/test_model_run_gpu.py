@@ -96,7 +96,7 @@ def calls(io=torch.bfloat16, shared=None):
     drafted = p[:, :K].argmax(-1).int()
     un, last = torch.full((B, K), 0.4, device="cuda"), torch.full((B,), 0.7, device="cuda")
     e = lambda *s, dtype=torch.float32: torch.empty(s, device="cuda", dtype=dtype)  # noqa: E731
-    o = dict(y=e(B, T, D, dtype=io), state=e(B, D), marks=e(B, -(-T // 64), D), yt=e(B, D, dtype=io), drate=e(D), drb=e(D),
+    o = dict(y=e(B, T, D, dtype=io), state=e(B, D), marks=e(B, -(-T // lh.GATED_MARK), D), yt=e(B, D, dtype=io), drate=e(D), drb=e(D),
              dib=e(D), dfirst=e(B, D), emb=e(n, D, dtype=io), dW=e(V, D), dW2=e(V, D), loss=e(7), lse=e(7), loss2=e(7),
              dl=e(7, V, dtype=io), dl2=e(7, V, dtype=io))
     o.update({k: e(B, T, D, dtype=io) for k in ("dr", "di", "du", "dz")})
