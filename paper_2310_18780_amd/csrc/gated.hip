@@ -4,17 +4,15 @@
 //   h <- a h + sqrt(1 - a^2) p u,   y = h (times z sigmoid(z))
 //
 // h after any run of steps is A h_before + H, with A the product of the run's decays and
-// H what its inputs alone leave.  A wavefront holds 64 channels of a row, one to a lane, and
-// takes 8 steps at a time, whose loads all start together.
+// H what its inputs alone leave.  A workgroup of 16 wavefronts holds 64 channels of a row, one
+// to a lane, and takes a block of 128 steps, 8 to a wavefront.  Each wavefront forms (A, H) of its
+// run, they meet in LDS, each chains those before its own to its entry state and walks its
+// steps again from registers: inputs are read once, outputs written once.  Where there are
+// rows enough a workgroup goes from block to block; else each block has a workgroup, which
+// leaves what its block alone does to a state as soon as it knows that, and finds the state
+// before it by looking back at the blocks before.
 //
-// Many rows: a workgroup of 16 wavefronts walks a prompt in blocks of 128 steps, 8 to a
-// wavefront.  Each forms (A, H) of its run, they meet in LDS, each chains those before its own
-// to its entry state and walks its steps again from registers: inputs are read once, outputs
-// written once.  Few rows: the prompt is cut into chunks, one to a wavefront that walks it by
-// itself; a first launch forms each chunk's (log2 A, H), and each chunk of the second folds those
-// before it.
-//
-// A run's decay is carried on as the sum of its logarithms (carry_on): products of roundings
+// A block's decay is carried on as the sum of its logarithms (carry_on): products of roundings
 // near 1 would be off by 2^-24 a step over thousands of steps.
 #include "gated_ops.hpp"
 
@@ -60,20 +58,94 @@ struct Run {
     }
 };
 
-template <typename T, bool GATE>
+// What blocks of a prompt hand on where each has a workgroup of its own: a word of 64 bits for
+// each channel and block, [B, blocks, D], written once and whole, so that a word that is not
+// empty is all there.  Block 0 and the last of every 16 leave the state after them (low half),
+// which the next blocks start from; the others the state that they alone leave and the log2 of
+// their decay, negated.
+constexpr int kGroup = 16;
+struct Links {
+    uint64_t* words;
+    uint32_t* ticket;
+};
+constexpr uint64_t kEmpty = ~uint64_t(0);
+
+__device__ __forceinline__ void post(uint64_t* p, float low, float high)
+{
+    const uint32_t h = __float_as_uint(high);
+    // (a NaN of all ones would read as empty)
+    const uint64_t w = uint64_t(h == ~0u ? 0x7fc00000u : h) << 32 | __float_as_uint(low);
+    __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t peek(const uint64_t* p)
+{
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float low_of(uint64_t w) { return __uint_as_float(uint32_t(w)); }
+__device__ __forceinline__ float high_of(uint64_t w) { return __uint_as_float(uint32_t(w >> 32)); }
+
+__global__ __launch_bounds__(256) void links_kernel(Links links, int64_t words)
+{
+    const int64_t step = int64_t(gridDim.x) * 256;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < words; i += step) links.words[i] = kEmpty;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *links.ticket = 0;
+}
+
+// The state before block k > 0: from the nearest block before it that leaves one, and those
+// between, each by the decays after it, always in the same order.  A block is started after all
+// before it (tickets), and block 0 waits for none, so that every wait ends.
+__device__ __forceinline__ float look_back(const uint64_t* words, int64_t k, int64_t D)
+{
+    constexpr int kLook = 4;  // words loaded together
+    const int64_t from = k < kGroup ? 0 : k / kGroup * kGroup - 1;
+    float h = 0.f, decay = 0.f;
+    for (int64_t j = k - 1; j >= from;) {
+        uint64_t w[kLook];
+#pragma unroll
+        for (int i = 0; i < kLook; ++i) w[i] = peek(words + (j - i > from ? j - i : from) * D);
+        const int64_t j0 = j;
+        bool wait = false;
+#pragma unroll
+        for (int i = 0; i < kLook; ++i) {
+            wait = wait || !__all(w[i] != kEmpty);
+            if (!wait && j0 - i >= from) {
+                h = fmaf(exp2_fast(-decay), low_of(w[i]), h);
+                decay += high_of(w[i]);
+                --j;
+            }
+        }
+        if (wait) __builtin_amdgcn_s_sleep(1);
+    }
+    return h;
+}
+
+// CHAIN: a workgroup to each block of each tile, else one to a tile, block after block.
+template <typename T, bool GATE, bool CHAIN>
 __global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, float* state, int resume,
-                                                              T* __restrict__ y, float* __restrict__ marks)
+                                                                 T* __restrict__ y, float* __restrict__ marks,
+                                                                 Links links)
 {
     __shared__ float2 runs[2][kWaves][kWave];
     __shared__ float logs[2][kWaves][kWave];
+    __shared__ float before[2][kWave];
+    __shared__ uint32_t ticket;
     const int lane = threadIdx.x % kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const Place at(in, blockIdx.x, 1, 0);
+    int64_t unit = blockIdx.x, k = 0;
+    if constexpr (CHAIN) {
+        if (threadIdx.x == 0) ticket = atomicAdd(links.ticket, 1u);
+        __syncthreads();
+        const uint32_t id = __builtin_amdgcn_readfirstlane(ticket), all = uint32_t(in.B * in.tiles);
+        k = id / all;
+        unit = id % all;
+    }
+    const Place at(in, unit, 1, 0);
     const int64_t c = at.c0 + at.lc;
     const GateParams par(in, c);
-    float h = resume ? state[at.b * in.D + c] : 0.f;  // before the block
+    float h = resume && k == 0 ? state[at.b * in.D + c] : 0.f;  // before the block
     int turn = 0;
-    for (int64_t tb = 0; tb < at.te; tb += kSpan, turn ^= 1) {
+    const int64_t first = k * kSpan, end = CHAIN ? first + kSpan : at.te;
+    for (int64_t tb = first; tb < end; tb += kSpan, turn ^= 1) {
         const int64_t t = tb + wave * kRun;
         const int m = int(at.te - t < kRun ? at.te - t : kRun);  // steps (<= 0: none)
         const Run<T, GATE> x(in, at, t, m);
@@ -90,14 +162,45 @@ __global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, 
         runs[turn][wave][lane] = make_float2(exp2_fast(-L), H);
         logs[turn][wave][lane] = L;
         __syncthreads();
-        // from zero: the states and decays before this run, and of the whole block
-        float e = 0.f, le = 0.f, end = 0.f, lend = 0.f;
-#pragma unroll 4
-        for (int j = 0; j < kWaves; ++j) {
-            if (j == wave) e = end, le = lend;
+        // states and decays before this run, from zero
+        float e = 0.f, le = 0.f;
+        auto chain = [&](int j) {
             const float2 n = runs[turn][j][lane];
-            end = fmaf(n.x, end, n.y);
-            lend += logs[turn][j][lane];
+            e = fmaf(n.x, e, n.y);
+            le += logs[turn][j][lane];
+        };
+        if (wave >= 8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) chain(j);
+        }
+        if (wave & 4) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) chain((wave & 8) + j);
+        }
+        if (wave & 2) {
+            chain(wave & 12);
+            chain((wave & 12) + 1);
+        }
+        if (wave & 1) chain(wave & 14);
+        // the last wavefront knows the whole block
+        const float lend = le + L, hend = fmaf(exp2_fast(-L), e, H);
+        if constexpr (CHAIN) {
+            if (wave == kWaves - 1) {
+                uint64_t* words = links.words + at.b * in.chunks * in.D + c;
+                const bool last = k == in.chunks - 1, leaves = k == 0 || k % kGroup == kGroup - 1;
+                if (!last && !leaves) post(words + k * in.D, hend, lend);
+                if (k > 0) h = look_back(words, k, in.D);
+                const float after = carry_on(h, lend, hend);
+                if (last)
+                    state[at.b * in.D + c] = after;
+                else if (leaves)
+                    post(words + k * in.D, after, 0.f);
+                before[0][lane] = h;
+            }
+            __syncthreads();
+            h = before[0][lane];
+        } else {
+            if (tb > 0) h = before[turn][lane];
         }
         float o = wave == 0 ? h : fmaf(exp2_fast(-le), h, e);
         if (marks && m > 0) marks[(at.b * in.marks + t / kRun) * in.D + c] = o;
@@ -107,64 +210,15 @@ __global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, 
             o = fmaf(a[s], o, v[s]);
             by.store(s, at.lc * uint32_t(sizeof(T)), x.out(s, o));
         }
-        h = carry_on(h, lend, end);
-    }
-    for (int64_t t = at.te + wave; t < in.T_; t += kWaves) io_store(y + (at.b * in.T_ + t) * in.D + c, 0.f);
-    if (wave == 0) state[at.b * in.D + c] = h;
-}
-
-constexpr int kWalkWaves = 4;  // wavefronts of a workgroup, each with a chunk of its own
-
-// ENDS: the chunks' ends only, into slots 1 .. of ends [B, chunks, D] (log2 of the decay,
-// negated, and state from zero); slot 0 holds the start.
-template <typename T, bool GATE, bool ENDS>
-__global__ __launch_bounds__(kWalkWaves* kWave) void gated_walk_kernel(
-    GatedIn<T> in, float* state, int resume, T* __restrict__ y, float* __restrict__ marks,
-    float2* __restrict__ ends, int64_t units)
-{
-    const int64_t unit = int64_t(blockIdx.x) * kWalkWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    if (unit >= units) return;
-    const Place at(in, unit, ENDS ? in.chunks - 1 : in.chunks, 0);
-    const int64_t c = at.c0 + at.lc;
-    const GateParams par(in, c);
-    float h = 0.f, total = 0.f;  // state; log2 of the decays so far, negated
-    float2* pe = ends + at.b * in.chunks * in.D + c;
-    if constexpr (ENDS) {
-        if (at.k == 0) pe[0] = make_float2(0.f, resume ? state[at.b * in.D + c] : 0.f);
-    } else if (in.chunks == 1) {
-        if (resume) h = state[at.b * in.D + c];
-    } else if (at.t0 < at.te || at.k == in.chunks - 1) {
-        for (int64_t j = 0; j <= at.k; ++j) {
-            const float2 v = pe[j * in.D];
-            h = carry_on(h, v.x, v.y);
+        if (!CHAIN && wave == kWaves - 1) {
+            h = carry_on(h, lend, hend);
+            before[turn ^ 1][lane] = h;
         }
     }
-    for (int64_t t = at.t0; t < at.te; t += kRun) {
-        const int m = int(at.te - t < kRun ? at.te - t : kRun);
-        const Run<T, GATE && !ENDS> x(in, at, t, m);
-        if (!ENDS && marks) marks[(at.b * in.marks + t / kRun) * in.D + c] = h;
-        float H = 0.f, L = 0.f, o = h;
-        const Rows<T> by(y + (at.b * in.T_ + t) * in.D + at.c0, in.D, at.wide, m);
-#pragma unroll
-        for (int s = 0; s < kRun; ++s) {
-            const GateStep g = x.step(s, m, par);
-            L += g.l;
-            H = fmaf(g.a, H, g.v);
-            if constexpr (!ENDS) {
-                o = fmaf(g.a, o, g.v);
-                by.store(s, at.lc * uint32_t(sizeof(T)), x.out(s, o));
-            }
-        }
-        h = carry_on(h, L, H);
-        total += L;
-    }
-    if constexpr (ENDS) {
-        pe[(at.k + 1) * in.D] = make_float2(total, h);
-    } else {
-        for (int64_t t = at.te > at.t0 ? at.te : at.t0; t < at.t1; ++t)
-            io_store(y + (at.b * in.T_ + t) * in.D + c, 0.f);
-        if (at.k == in.chunks - 1) state[at.b * in.D + c] = h;
-    }
+    const int64_t t1 = CHAIN && first + kSpan < in.T_ ? first + kSpan : in.T_;
+    for (int64_t t = (at.te > first ? at.te : first) + wave; t < t1; t += kWaves)
+        io_store(y + (at.b * in.T_ + t) * in.D + c, 0.f);
+    if (!CHAIN && wave == kWaves - 1) state[at.b * in.D + c] = h;
 }
 
 // One token per row.
@@ -189,32 +243,26 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedIn<T> in, float* _
     io_store(y + b * in.D + c, o);
 }
 
-// Workgroups of 16 wavefronts from here on (half again as many as CUs).
-constexpr int64_t kManyTiles = 384;
-
 template <typename T, bool GATE>
-hipError_t gated(const Gated& g, float* state, bool resume, T* y, float* marks, float2* ends,
+hipError_t gated(const Gated& g, float* state, bool resume, T* y, float* marks, void* workspace,
                  hipStream_t stream)
 {
     const GatedPlan p = gated_plan(g.B, g.T, g.D);
     const GatedIn<T> in = gated_in<T>(g, p);
-    const int64_t tiles = gated_tiles(g.B, g.D);
-    if (tiles >= kManyTiles) {
-        hipLaunchKernelGGL((gated_kernel<T, GATE>), dim3(uint32_t(tiles)), dim3(kWaves * kWave), 0, stream, in,
-                           state, int(resume), y, marks);
+    const dim3 grid(uint32_t(g.B * in.tiles * p.chunks)), block(kWaves * kWave);
+    Links links{};
+    if (p.chunks == 1) {
+        hipLaunchKernelGGL((gated_kernel<T, GATE, false>), grid, block, 0, stream, in, state, int(resume), y,
+                           marks, links);
         return hipGetLastError();
     }
-    const dim3 block(kWalkWaves * kWave);
-    auto grid = [](int64_t units) { return dim3(uint32_t((units + kWalkWaves - 1) / kWalkWaves)); };
-    if (p.chunks > 1) {
-        const int64_t units = tiles * (p.chunks - 1);
-        hipLaunchKernelGGL((gated_walk_kernel<T, GATE, true>), grid(units), block, 0, stream, in, state,
-                           int(resume), static_cast<T*>(nullptr), static_cast<float*>(nullptr), ends, units);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
-    const int64_t units = tiles * p.chunks;
-    hipLaunchKernelGGL((gated_walk_kernel<T, GATE, false>), grid(units), block, 0, stream, in, state, int(resume),
-                       y, marks, ends, units);
+    const int64_t words = g.B * p.chunks * g.D;
+    links.words = static_cast<uint64_t*>(workspace);
+    links.ticket = reinterpret_cast<uint32_t*>(links.words + words);
+    const int64_t fills = (words + 1023) / 1024;
+    hipLaunchKernelGGL(links_kernel, dim3(uint32_t(fills < 1024 ? fills : 1024)), dim3(256), 0, stream, links, words);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL((gated_kernel<T, GATE, true>), grid, block, 0, stream, in, state, int(resume), y, marks, links);
     return hipGetLastError();
 }
 
@@ -222,17 +270,19 @@ hipError_t gated(const Gated& g, float* state, bool resume, T* y, float* marks, 
 
 GatedPlan gated_plan(int64_t B, int64_t T, int64_t D)
 {
-    const int64_t tiles = gated_tiles(B, D);
-    if (tiles >= kManyTiles) return GatedPlan{T > 0 ? T : 1, 1, 0};
-    GatedPlan p = gated_chunks(B, T, D, 4096, 64);
-    p.ws_bytes = p.chunks > 1 ? sizeof(float2) * size_t(B) * p.chunks * D : 0;
+    GatedPlan p{T > 0 ? T : 1, 1, 0};  // (every workgroup sees the whole prompt)
+    const int64_t blocks = (T + kSpan - 1) / kSpan;
+    // half again as many tiles as CUs fill the GPU by themselves
+    if (gated_tiles(B, D) < 384 && blocks > 1) {
+        p.chunks = blocks;
+        p.ws_bytes = sizeof(uint64_t) * size_t(B) * blocks * D + 256;
+    }
     return p;
 }
 
 int64_t gated_threads(int64_t B, int64_t T, int64_t D)
 {
-    const int64_t tiles = gated_tiles(B, D);
-    return tiles >= kManyTiles ? tiles * kWaves * kWave : (tiles * gated_plan(B, T, D).chunks + kWalkWaves) * kWave;
+    return gated_tiles(B, D) * gated_plan(B, T, D).chunks * kWaves * kWave;
 }
 
 int64_t gated_step_threads(int64_t B, int64_t D) { return B * ((D + 255) / 256) * 256; }
@@ -240,12 +290,11 @@ int64_t gated_step_threads(int64_t B, int64_t D) { return B * ((D + 255) / 256) 
 hipError_t launch_gated(const Gated& g, float* state, bool resume, void* y, float* marks,
                         void* workspace, hipStream_t stream)
 {
-    float2* ends = static_cast<float2*>(workspace);
     if (g.bf16_io)
-        return g.z ? gated<bf16, true>(g, state, resume, static_cast<bf16*>(y), marks, ends, stream)
-                   : gated<bf16, false>(g, state, resume, static_cast<bf16*>(y), marks, ends, stream);
-    return g.z ? gated<float, true>(g, state, resume, static_cast<float*>(y), marks, ends, stream)
-               : gated<float, false>(g, state, resume, static_cast<float*>(y), marks, ends, stream);
+        return g.z ? gated<bf16, true>(g, state, resume, static_cast<bf16*>(y), marks, workspace, stream)
+                   : gated<bf16, false>(g, state, resume, static_cast<bf16*>(y), marks, workspace, stream);
+    return g.z ? gated<float, true>(g, state, resume, static_cast<float*>(y), marks, workspace, stream)
+               : gated<float, false>(g, state, resume, static_cast<float*>(y), marks, workspace, stream);
 }
 
 hipError_t launch_gated_step(const Gated& g, float* state, void* y_t, hipStream_t stream)

@@ -95,11 +95,15 @@ __global__ __launch_bounds__(kWaves* kWave, 6) void gated_grad_kernel(GatedIn<T>
     const int64_t c = at.c0 + at.lc, rows = at.b * in.T_ * in.D;
     const uint32_t lane = at.lc * uint32_t(sizeof(T));
     const GateParams par(in, c);
-    float X = out.dlast ? out.dlast[at.b * in.D + c] : 0.f;
-    for (int64_t j = in.chunks - 1; j > at.k; --j) {
+    // the chunks after, each by the decays before it
+    float X = 0.f, decay = 0.f;
+#pragma unroll 4
+    for (int64_t j = at.k + 1; j < in.chunks; ++j) {
         const float2 e = ends[(at.b * in.chunks + j) * in.D + c];
-        X = carry_on(X, e.x, e.y);
+        X = fmaf(exp2_fast(-decay), e.y, X);
+        decay += e.x;
     }
+    if (out.dlast) X = fmaf(exp2_fast(-decay), out.dlast[at.b * in.D + c], X);
     float sum_rate = 0.f, sum_r = 0.f, sum_i = 0.f;
     for (int64_t t = at.last_run(); t >= at.t0; t -= kRun) {
         const int m = int(at.te - t < kRun ? at.te - t : kRun);

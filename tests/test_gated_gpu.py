@@ -74,7 +74,7 @@ def ref_args(c):
 
 
 SHAPES = [(1, 1, 1), (1, 2, 3), (2, 7, 64), (3, 64, 65), (2, 65, 70), (1, 127, 130), (1, 128, 64), (2, 129, 67), (1, 700, 100),
-          (5, 300, 33), (400, 3, 64), (2, 1025, 5)]
+          (5, 300, 33), (400, 3, 64), (2, 1025, 5), (390, 140, 10)]
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
