@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kWaves = 16;
 constexpr int kSpan = kWaves * kRun;  // steps of a block
+constexpr int64_t kGroups = 512;  // workgroups that fill the GPU
 
 // The inputs of a run, as they lie in memory.
 template <typename T, bool GATE>
@@ -58,7 +59,7 @@ struct Run {
     }
 };
 
-// What blocks of a prompt hand on where each has a workgroup of its own: a word of 64 bits for
+// What blocks of a prompt hand on where several workgroups share a tile: a word of 64 bits for
 // each channel and block, [B, blocks, D], written once and whole, so that a word that is not
 // empty is all there.  Block 0 and the last of every 16 leave the state after them (low half),
 // which the next blocks start from; the others the state that they alone leave and the log2 of
@@ -66,7 +67,7 @@ struct Run {
 constexpr int kGroup = 16;
 struct Links {
     uint64_t* words;
-    uint32_t* ticket;
+    uint32_t* tickets;  // [B, tiles]: blocks that are taken
 };
 constexpr uint64_t kEmpty = ~uint64_t(0);
 
@@ -84,16 +85,17 @@ __device__ __forceinline__ uint64_t peek(const uint64_t* p)
 __device__ __forceinline__ float low_of(uint64_t w) { return __uint_as_float(uint32_t(w)); }
 __device__ __forceinline__ float high_of(uint64_t w) { return __uint_as_float(uint32_t(w >> 32)); }
 
-__global__ __launch_bounds__(256) void links_kernel(Links links, int64_t words)
+__global__ __launch_bounds__(256) void links_kernel(Links links, int64_t words, int64_t tiles)
 {
     const int64_t step = int64_t(gridDim.x) * 256;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < words; i += step) links.words[i] = kEmpty;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *links.ticket = 0;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < tiles; i += step) links.tickets[i] = 0;
 }
 
 // The state before block k > 0: from the nearest block before it that leaves one, and those
-// between, each by the decays after it, always in the same order.  A block is started after all
-// before it (tickets), and block 0 waits for none, so that every wait ends.
+// between, each by the decays after it, always in the same order.  Blocks are taken in their order
+// and a workgroup finishes one before it begins the next that it has taken, so the first unfinished
+// block of a tile is always at work and has none to wait for: every wait ends.
 __device__ __forceinline__ float look_back(const uint64_t* words, int64_t k, int64_t D)
 {
     constexpr int kLook = 4;  // words loaded together
@@ -119,7 +121,7 @@ __device__ __forceinline__ float look_back(const uint64_t* words, int64_t k, int
     return h;
 }
 
-// CHAIN: a workgroup to each block of each tile, else one to a tile, block after block.
+// CHAIN: the workgroups of a tile take its blocks in turn, else one takes them all.
 template <typename T, bool GATE, bool CHAIN>
 __global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, float* state, int resume,
                                                                  T* __restrict__ y, float* __restrict__ marks,
@@ -128,24 +130,25 @@ __global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, 
     __shared__ float2 runs[2][kWaves][kWave];
     __shared__ float logs[2][kWaves][kWave];
     __shared__ float before[2][kWave];
-    __shared__ uint32_t ticket;
+    __shared__ uint32_t taken[2];
     const int lane = threadIdx.x % kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    int64_t unit = blockIdx.x, k = 0;
+    const uint32_t unit = CHAIN ? blockIdx.x % uint32_t(in.B * in.tiles) : blockIdx.x;
+    uint32_t k = 0;
     if constexpr (CHAIN) {
-        if (threadIdx.x == 0) ticket = atomicAdd(links.ticket, 1u);
+        if (threadIdx.x == 0) taken[0] = atomicAdd(links.tickets + unit, 1u);
         __syncthreads();
-        const uint32_t id = __builtin_amdgcn_readfirstlane(ticket), all = uint32_t(in.B * in.tiles);
-        k = id / all;
-        unit = id % all;
+        k = __builtin_amdgcn_readfirstlane(taken[0]);
     }
     const Place at(in, unit, 1, 0);
     const int64_t c = at.c0 + at.lc;
     const GateParams par(in, c);
-    float h = resume && k == 0 ? state[at.b * in.D + c] : 0.f;  // before the block
+    const uint32_t blocks = at.te > 0 ? uint32_t((at.te + kSpan - 1) / kSpan) : 1;  // with tokens
+    float h = resume ? state[at.b * in.D + c] : 0.f;  // before the block
     int turn = 0;
-    const int64_t first = k * kSpan, end = CHAIN ? first + kSpan : at.te;
-    for (int64_t tb = first; tb < end; tb += kSpan, turn ^= 1) {
+    for (; k < blocks; turn ^= 1) {
+        const int64_t tb = int64_t(k) * kSpan;
+        if (CHAIN && threadIdx.x == 0) taken[turn ^ 1] = atomicAdd(links.tickets + unit, 1u);
         const int64_t t = tb + wave * kRun;
         const int m = int(at.te - t < kRun ? at.te - t : kRun);  // steps (<= 0: none)
         const Run<T, GATE> x(in, at, t, m);
@@ -184,10 +187,11 @@ __global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, 
         if (wave & 1) chain(wave & 14);
         // the last wavefront knows the whole block
         const float lend = le + L, hend = fmaf(exp2_fast(-L), e, H);
+        const bool last = k == blocks - 1;
         if constexpr (CHAIN) {
             if (wave == kWaves - 1) {
                 uint64_t* words = links.words + at.b * in.chunks * in.D + c;
-                const bool last = k == in.chunks - 1, leaves = k == 0 || k % kGroup == kGroup - 1;
+                const bool leaves = k == 0 || k % kGroup == kGroup - 1;
                 if (!last && !leaves) post(words + k * in.D, hend, lend);
                 if (k > 0) h = look_back(words, k, in.D);
                 const float after = carry_on(h, lend, hend);
@@ -195,12 +199,12 @@ __global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, 
                     state[at.b * in.D + c] = after;
                 else if (leaves)
                     post(words + k * in.D, after, 0.f);
-                before[0][lane] = h;
+                before[turn][lane] = h;
             }
             __syncthreads();
-            h = before[0][lane];
+            h = before[turn][lane];
         } else {
-            if (tb > 0) h = before[turn][lane];
+            if (k > 0) h = before[turn][lane];
         }
         float o = wave == 0 ? h : fmaf(exp2_fast(-le), h, e);
         if (marks && m > 0) marks[(at.b * in.marks + t / kRun) * in.D + c] = o;
@@ -212,13 +216,15 @@ __global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, 
         }
         if (!CHAIN && wave == kWaves - 1) {
             h = carry_on(h, lend, hend);
+            if (last) state[at.b * in.D + c] = h;
             before[turn ^ 1][lane] = h;
         }
+        k = CHAIN ? __builtin_amdgcn_readfirstlane(taken[turn ^ 1]) : k + 1;
     }
-    const int64_t t1 = CHAIN && first + kSpan < in.T_ ? first + kSpan : in.T_;
-    for (int64_t t = (at.te > first ? at.te : first) + wave; t < t1; t += kWaves)
+    const int64_t share = CHAIN ? blockIdx.x / uint32_t(in.B * in.tiles) : 0;
+    const int64_t shares = CHAIN ? gridDim.x / uint32_t(in.B * in.tiles) : 1;
+    for (int64_t t = at.te + share * kWaves + wave; t < in.T_; t += shares * kWaves)
         io_store(y + (at.b * in.T_ + t) * in.D + c, 0.f);
-    if (!CHAIN && wave == kWaves - 1) state[at.b * in.D + c] = h;
 }
 
 // One token per row.
@@ -243,26 +249,36 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedIn<T> in, float* _
     io_store(y + b * in.D + c, o);
 }
 
+// Workgroups that share a tile: one where there are tiles enough, or blocks too few.
+int64_t gated_shares(int64_t tiles, int64_t blocks)
+{
+    if (tiles >= kGroups * 3 / 4 || blocks < 2) return 1;
+    const int64_t n = (kGroups + tiles - 1) / tiles;
+    return n < blocks ? n : blocks;
+}
+
 template <typename T, bool GATE>
 hipError_t gated(const Gated& g, float* state, bool resume, T* y, float* marks, void* workspace,
                  hipStream_t stream)
 {
     const GatedPlan p = gated_plan(g.B, g.T, g.D);
     const GatedIn<T> in = gated_in<T>(g, p);
-    const dim3 grid(uint32_t(g.B * in.tiles * p.chunks)), block(kWaves * kWave);
+    const int64_t tiles = g.B * in.tiles;
+    const dim3 block(kWaves * kWave);
     Links links{};
-    if (p.chunks == 1) {
-        hipLaunchKernelGGL((gated_kernel<T, GATE, false>), grid, block, 0, stream, in, state, int(resume), y,
-                           marks, links);
+    if (p.ws_bytes == 0) {
+        hipLaunchKernelGGL((gated_kernel<T, GATE, false>), dim3(uint32_t(tiles)), block, 0, stream, in, state,
+                           int(resume), y, marks, links);
         return hipGetLastError();
     }
-    const int64_t words = g.B * p.chunks * g.D;
+    const int64_t words = g.B * p.chunks * g.D, fills = (words + 1023) / 1024;
     links.words = static_cast<uint64_t*>(workspace);
-    links.ticket = reinterpret_cast<uint32_t*>(links.words + words);
-    const int64_t fills = (words + 1023) / 1024;
-    hipLaunchKernelGGL(links_kernel, dim3(uint32_t(fills < 1024 ? fills : 1024)), dim3(256), 0, stream, links, words);
+    links.tickets = reinterpret_cast<uint32_t*>(links.words + words);
+    hipLaunchKernelGGL(links_kernel, dim3(uint32_t(fills < 1024 ? fills : 1024)), dim3(256), 0, stream, links, words,
+                       tiles);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL((gated_kernel<T, GATE, true>), grid, block, 0, stream, in, state, int(resume), y, marks, links);
+    hipLaunchKernelGGL((gated_kernel<T, GATE, true>), dim3(uint32_t(tiles * gated_shares(tiles, p.chunks))), block, 0,
+                       stream, in, state, int(resume), y, marks, links);
     return hipGetLastError();
 }
 
@@ -270,19 +286,18 @@ hipError_t gated(const Gated& g, float* state, bool resume, T* y, float* marks, 
 
 GatedPlan gated_plan(int64_t B, int64_t T, int64_t D)
 {
-    GatedPlan p{T > 0 ? T : 1, 1, 0};  // (every workgroup sees the whole prompt)
-    const int64_t blocks = (T + kSpan - 1) / kSpan;
-    // half again as many tiles as CUs fill the GPU by themselves
-    if (gated_tiles(B, D) < 384 && blocks > 1) {
-        p.chunks = blocks;
-        p.ws_bytes = sizeof(uint64_t) * size_t(B) * blocks * D + 256;
-    }
+    // (every workgroup sees the whole prompt)
+    GatedPlan p{T > 0 ? T : 1, T > 0 ? (T + kSpan - 1) / kSpan : 1, 0};
+    const int64_t tiles = gated_tiles(B, D);
+    if (gated_shares(tiles, p.chunks) > 1)
+        p.ws_bytes = (sizeof(uint64_t) * size_t(B) * p.chunks * D + sizeof(uint32_t) * size_t(tiles) + 7) / 8 * 8;
     return p;
 }
 
 int64_t gated_threads(int64_t B, int64_t T, int64_t D)
 {
-    return gated_tiles(B, D) * gated_plan(B, T, D).chunks * kWaves * kWave;
+    const int64_t tiles = gated_tiles(B, D);
+    return tiles * gated_shares(tiles, gated_plan(B, T, D).chunks) * kWaves * kWave;
 }
 
 int64_t gated_step_threads(int64_t B, int64_t D) { return B * ((D + 255) / 256) * 256; }

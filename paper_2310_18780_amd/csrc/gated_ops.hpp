@@ -99,9 +99,11 @@ struct Place {
     __device__ __forceinline__ Place(const GatedIn<T>& in, int64_t unit, int64_t chunks, int64_t first)
     {
         const int lane = threadIdx.x % kWave;
-        c0 = unit % in.tiles * kTile;
-        k = unit / in.tiles % chunks + first;
-        b = unit / in.tiles / chunks;
+        // (a launch has fewer than 2^32 threads)
+        const uint32_t u = uint32_t(unit), tiles = uint32_t(in.tiles), row = u / tiles;
+        c0 = int64_t(u - row * tiles) * kTile;
+        b = row / uint32_t(chunks);
+        k = row - uint32_t(b) * uint32_t(chunks) + first;
         wide = int(in.D - c0 < kTile ? in.D - c0 : kTile);
         lc = uint32_t(lane < wide ? lane : wide - 1);
         const int64_t n = gated_length(in.lengths, b, in.T_);
