@@ -21,7 +21,6 @@
 namespace lh {
 namespace {
 
-constexpr int64_t kMaxBlocks = 1 << 20;  // grid-stride beyond
 constexpr int kHold = 16;  // pieces of a row that a thread holds
 
 constexpr float kNone = -__builtin_inff();
@@ -30,6 +29,21 @@ __device__ __forceinline__ float wave_max(float v)
 {
     for (int o = 1; o < kWave; o *= 2) v = fmaxf(v, __shfl_xor(v, o, kWave));
     return v;
+}
+
+// A row's pieces stay as they lie in memory from one pass to the next: the values that they
+// expand to, and exponentials of those, would take four times the registers.
+template <typename R>
+__device__ __forceinline__ void forget(R& r)
+{
+    if constexpr (sizeof(R) == 16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t x = r[i];
+            asm("" : "+v"(x));
+            r[i] = x;
+        }
+    }
 }
 
 template <typename T>
@@ -48,179 +62,161 @@ struct Args {
     int64_t ld_d;
 };
 
-// A row's pieces: the whole ones of a thread from registers (ITER > 0) or memory.
-// MODE 0: loss; 1: loss and gradient; 2: gradient from lse.
+// One row: MODE 0: loss; 1: loss and gradient; 2: gradient from lse.  A thread has ITER pieces of
+// the row in registers, or reads them again (ITER = 0), and at most one slot (K <= BLOCK).
 template <typename T, int BLOCK, int ITER, int MODE>
-__global__ __launch_bounds__(BLOCK) void distill_kernel(Args<T> a)
+__global__ __launch_bounds__(BLOCK, ITER <= 8 ? 8 : 4) void distill_kernel(Args<T> a)
 {
     constexpr int V = kVec<T>;
     constexpr int waves = BLOCK / kWave;
-    __shared__ float2 red[2][waves];
-    __shared__ float reds[waves];
-    __shared__ float2 slots[LH_DISTILL_MAX_TOP];  // id (bits), p
+    __shared__ float2 tops[waves];
+    __shared__ float4 sums[waves];
+    __shared__ float2 slots[BLOCK];  // id (bits), e
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t pieces = a.V / V, tail = a.V % V;  // whole pieces, then single values
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T* x = a.logits + row * a.ld;
-        T* out = MODE ? a.dlogits + row * a.ld_d : nullptr;
-        const float scale = a.scale ? a.scale[row] : 1.f;
-        // the teacher's side: one slot to a thread (K <= 1024, four to a thread of 256)
-        constexpr int S = LH_DISTILL_MAX_TOP / BLOCK;
-        float t[S];
-        int id[S];
-        float top_t = kNone;
+    const int pieces = int(a.V / V), tail = int(a.V % V);  // whole pieces, then single values
+    const int64_t row = blockIdx.x;
+    const T* x = a.logits + row * a.ld;
+    T* out = MODE ? a.dlogits + row * a.ld_d : nullptr;
+    const float scale = a.scale ? a.scale[row] : 1.f;
+
+    // the teacher's side: a slot to a thread
+    const bool has = int(threadIdx.x) < a.K;
+    int id = -1;
+    float t = kNone;
+    if (has) {
+        id = a.ids[row * a.K + threadIdx.x];
+        const float v = a.values[row * a.K + threadIdx.x];
+        // (NaN as infinity, which the maximum does not drop: the row is NaN)
+        if (id >= 0 && id < a.V) t = v != v ? -kNone : v;
+    }
+    // the student's: pieces and values past the last whole piece
+    Raw<T, V> raw[ITER > 0 ? ITER : 1];
+    float last = kNone, own = 0.f, top = kNone;
+    auto each = [&](auto f) __attribute__((always_inline)) {
+        if constexpr (ITER > 0) {
 #pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const int k = threadIdx.x + i * BLOCK;
-            t[i] = kNone;
-            id[i] = -1;
-            if (k < a.K) {
-                id[i] = a.ids[row * a.K + k];
-                const float v = a.values[row * a.K + k];
-                // (NaN as infinity, which the maximum does not drop: the row is NaN)
-                if (id[i] >= 0 && id[i] < a.V) t[i] = v != v ? -kNone : v;
+            for (int i = 0; i < ITER; ++i) {
+                const int p = i * BLOCK + int(threadIdx.x);
+                if (p < pieces) f(raw[i], p);
+                forget(raw[i]);
             }
-            top_t = fmaxf(top_t, t[i]);
+        } else {
+            for (int p = threadIdx.x; p < pieces; p += BLOCK) f(load_raw<V>(x + int64_t(p) * V), p);
         }
-        // the student's: pieces and values past the last whole piece
-        Raw<T, V> raw[ITER > 0 ? ITER : 1];
-        float last = kNone, top = kNone;
-        auto each = [&](auto f) {
-            if constexpr (ITER > 0) {
+    };
+    if (scale != 0.f) {
+        if constexpr (ITER > 0) {
 #pragma unroll
-                for (int i = 0; i < ITER; ++i) {
-                    const int64_t p = i * BLOCK + threadIdx.x;
-                    if (p < pieces) f(raw[i], p);
-                }
-            } else {
-                for (int64_t p = threadIdx.x; p < pieces; p += BLOCK) f(load_raw<V>(x + p * V), p);
-            }
-        };
-        if (scale != 0.f) {
-            if constexpr (ITER > 0) {
-#pragma unroll
-                for (int i = 0; i < ITER; ++i) {
-                    const int64_t p = i * BLOCK + threadIdx.x;
-                    if (p < pieces) raw[i] = load_raw<V>(x + p * V);
-                }
-            }
-            if (threadIdx.x < tail) last = io_load(x + pieces * V + threadIdx.x);
-            if constexpr (MODE < 2) {
-                top = last;
-                each([&](const Raw<T, V>& r, int64_t) {
-                    float v[V];
-                    expand<V, T>(r, v);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) top = fmaxf(top, v[j]);
-                });
+            for (int i = 0; i < ITER; ++i) {
+                const int p = i * BLOCK + int(threadIdx.x);
+                if (p < pieces) raw[i] = load_raw<V>(x + int64_t(p) * V);
             }
         }
-        top = wave_max(top);
-        top_t = wave_max(top_t);
-        __syncthreads();  // (the row before has been read from LDS)
-        if (lane == 0) red[0][wave] = make_float2(top, top_t);
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < waves; ++w) {
-            const float2 v = red[0][w];
-            top = fmaxf(top, v.x);
-            top_t = fmaxf(top_t, v.y);
-        }
-        const bool none = scale == 0.f || top_t == kNone;
-        if (none) {  // no slots, or a row that takes no part
-            if (threadIdx.x == 0) {
-                if (MODE < 2) a.loss[row] = 0.f;
-                if (MODE < 2 && a.lse_out) a.lse_out[row] = 0.f;
-            }
-            if constexpr (MODE > 0)
-                for (int64_t j = threadIdx.x; j < a.V; j += BLOCK) io_store(out + j, 0.f);
-            continue;
-        }
-        // exponents in base 2: less the row's largest (a difference first: the rounding of a
-        // product of a large offset would not cancel), or less lse
-        float off = MODE == 2 ? a.lse_in[row] * kLog2e : top;
-        if (off == kNone) off = 0.f;
-        auto power = [&](float v) { return MODE == 2 ? fmaf(v, a.to2, -off) : (v - off) * a.to2; };
-        float2 sum = make_float2(0.f, 0.f);  // of the student's exponentials, of the teacher's
-        float cross = 0.f, e[S], own[S];
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const float d = (t[i] - top_t) * a.to2;
-            e[i] = t[i] == kNone ? 0.f : exp2_fast(d);
-            own[i] = e[i] != 0.f ? power(io_load(x + id[i])) : 0.f;
-            sum.y += e[i];
-            cross += e[i] != 0.f ? e[i] * (d - own[i]) : 0.f;
-        }
+        if (int(threadIdx.x) < tail) last = io_load(x + int64_t(pieces) * V + threadIdx.x);
+        if (t != kNone) own = io_load(x + id);
         if constexpr (MODE < 2) {
-            if (threadIdx.x < tail) sum.x = exp2_fast(power(last));
-            each([&](const Raw<T, V>& r, int64_t) {
+            top = last;
+            each([&](const Raw<T, V>& r, int) {
                 float v[V];
                 expand<V, T>(r, v);
 #pragma unroll
-                for (int j = 0; j < V; ++j) sum.x += exp2_fast(power(v[j]));
+                for (int j = 0; j < V; j += 2) top = fmaxf(fmaxf(v[j], v[j + 1]), top);
             });
-            cross = wave_sum(cross);
-            sum.x = wave_sum(sum.x);
         }
-        sum.y = wave_sum(sum.y);
-        if (lane == 0) {
-            red[1][wave] = sum;
-            reds[wave] = cross;
-        }
-        __syncthreads();
-        sum = make_float2(0.f, 0.f);
-        cross = 0.f;
+    }
+    const float2 most = make_float2(wave_max(top), wave_max(t));
+    if (lane == 0) tops[wave] = most;
+    __syncthreads();
+    const float2 of_wave = tops[lane % waves];
+    top = of_wave.x;
+    float top_t = of_wave.y;
 #pragma unroll
-        for (int w = 0; w < waves; ++w) {
-            sum.x += red[1][w].x;
-            sum.y += red[1][w].y;
-            cross += reds[w];
-        }
+    for (int o = 1; o < waves; o *= 2) {
+        top = fmaxf(top, __shfl_xor(top, o, kWave));
+        top_t = fmaxf(top_t, __shfl_xor(top_t, o, kWave));
+    }
+    if (scale == 0.f || top_t == kNone) {  // a row that takes no part, or without slots
         if (MODE < 2 && threadIdx.x == 0) {
-            const float l2 = __builtin_amdgcn_logf(sum.x);
-            // (no finite logit: the student's probabilities are 0)
-            const float nats = sum.x == 0.f ? __builtin_inff()
-                                            : kLn2 * (cross / sum.y + (l2 - __builtin_amdgcn_logf(sum.y)));
-            a.loss[row] = scale * a.tau * a.tau * nats;
-            if (a.lse_out) a.lse_out[row] = fmaf(kLn2, l2, top == kNone ? kNone : top / a.tau);
+            a.loss[row] = 0.f;
+            if (a.lse_out) a.lse_out[row] = 0.f;
         }
         if constexpr (MODE > 0) {
-            float c = scale * a.tau;
-            if (MODE == 2) c *= a.dloss[row];
-            const float cq = MODE == 2 ? c : sum.x == 0.f ? 0.f : c / sum.x;
-            const float rp = 1.f / sum.y;
+            const float zeros[V] = {};
+            for (int p = threadIdx.x; p < pieces; p += BLOCK) put<V>(out + int64_t(p) * V, zeros);
+            if (int(threadIdx.x) < tail) io_store(out + int64_t(pieces) * V + threadIdx.x, 0.f);
+        }
+        return;
+    }
+    // exponents in base 2: less the row's largest (a difference first: the rounding of a product of
+    // a large offset would not cancel), or less lse
+    float off = MODE == 2 ? a.lse_in[row] * kLog2e : top;
+    if (off == kNone) off = 0.f;
+    auto power = [&](float v) { return MODE == 2 ? fmaf(v, a.to2, -off) : (v - off) * a.to2; };
+    const float d = (t - top_t) * a.to2;
+    const float e = t == kNone ? 0.f : exp2_fast(d);
+    own = power(own);
+    if (MODE > 0 && has) slots[threadIdx.x] = make_float2(__int_as_float(id), e);
+    // of the student's exponentials, of the teacher's, and of those times both exponents' distance
+    float4 sum = make_float4(0.f, e, e != 0.f ? e * (d - own) : 0.f, 0.f);
+    if constexpr (MODE < 2) {
+        if (int(threadIdx.x) < tail) sum.x = exp2_fast(power(last));
+        each([&](const Raw<T, V>& r, int) {
+            float v[V];
+            expand<V, T>(r, v);
 #pragma unroll
-            for (int i = 0; i < S; ++i) {
-                const int k = threadIdx.x + i * BLOCK;
-                if (k < a.K) slots[k] = make_float2(__int_as_float(t[i] == kNone ? -1 : id[i]), e[i] * rp);
-            }
-            each([&](const Raw<T, V>& r, int64_t p) {
-                float v[V];
-                expand<V, T>(r, v);
+            for (int j = 0; j < V; ++j) sum.x += exp2_fast(power(v[j]));
+        });
+        sum.x = wave_sum(sum.x);
+        sum.z = wave_sum(sum.z);
+    }
+    sum.y = wave_sum(sum.y);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = sums[lane % waves];
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] = exp2_fast(power(v[j])) * cq;
-                put<V>(out + p * V, v);
-            });
-            if (threadIdx.x < tail)
-                io_store(out + pieces * V + threadIdx.x, exp2_fast(power(last)) * cq);
-            __syncthreads();
+    for (int o = 1; o < waves; o *= 2) {
+        sum.x += __shfl_xor(sum.x, o, kWave);
+        sum.y += __shfl_xor(sum.y, o, kWave);
+        sum.z += __shfl_xor(sum.z, o, kWave);
+    }
+    if (MODE < 2 && threadIdx.x == 0) {
+        const float l2 = __builtin_amdgcn_logf(sum.x);
+        // (no finite logit: the student's probabilities are 0)
+        const float nats = sum.x == 0.f ? __builtin_inff()
+                                        : kLn2 * (sum.z / sum.y + (l2 - __builtin_amdgcn_logf(sum.y)));
+        a.loss[row] = scale * a.tau * a.tau * nats;
+        if (a.lse_out) a.lse_out[row] = fmaf(kLn2, l2, top == kNone ? kNone : top / a.tau);
+    }
+    if constexpr (MODE > 0) {
+        float c = scale * a.tau;
+        if (MODE == 2) c *= a.dloss[row];
+        const float cq = MODE == 2 ? c : sum.x == 0.f ? 0.f : c / sum.x;
+        each([&](const Raw<T, V>& r, int p) {
+            float v[V];
+            expand<V, T>(r, v);
 #pragma unroll
-            for (int i = 0; i < S; ++i) {
-                if (e[i] == 0.f) continue;
-                float p = 0.f;
-                for (int k = 0; k < a.K; ++k) {
-                    const float2 s = slots[k];
-                    p += __float_as_int(s.x) == id[i] ? s.y : 0.f;
-                }
-                io_store(out + id[i], fmaf(exp2_fast(own[i]), cq, -c * p));
+            for (int j = 0; j < V; ++j) v[j] = exp2_fast(power(v[j])) * cq;
+            put<V>(out + int64_t(p) * V, v);
+        });
+        if (int(threadIdx.x) < tail)
+            io_store(out + int64_t(pieces) * V + threadIdx.x, exp2_fast(power(last)) * cq);
+        // a slot's own value: the exponentials of all slots of its id, in their order
+        float of_id = 0.f;
+        if (e != 0.f) {
+#pragma unroll 8
+            for (int k = 0; k < a.K; ++k) {
+                const float2 s = slots[k];
+                of_id += __float_as_int(s.x) == id ? s.y : 0.f;
             }
         }
+        __syncthreads();
+        if (e != 0.f) io_store(out + id, fmaf(exp2_fast(own), cq, -c * (of_id / sum.y)));
     }
 }
 
 // Threads to a row and pieces of a thread (0: read again from memory).
 template <int MODE, typename T, typename F>
-hipError_t with_shape(int64_t V, F f)
+hipError_t with_shape(int64_t V, int K, F f)
 {
     const int64_t pieces = V / kVec<T>;
     auto iters = [&](auto block) {
@@ -229,12 +225,14 @@ hipError_t with_shape(int64_t V, F f)
         if (n <= 1) return f(block, std::integral_constant<int, 1>());
         if (n <= 2) return f(block, std::integral_constant<int, 2>());
         if (n <= 4) return f(block, std::integral_constant<int, 4>());
-        if (n <= 8) return f(block, std::integral_constant<int, 8>());
-        if constexpr (B == 1024)
+        if constexpr (B == 1024) {
+            if (n <= 6) return f(block, std::integral_constant<int, 6>());
+            if (n <= 8) return f(block, std::integral_constant<int, 8>());
             if (n <= kHold) return f(block, std::integral_constant<int, kHold>());
+        }
         return f(block, std::integral_constant<int, 0>());
     };
-    if (pieces <= 4 * 256) return iters(std::integral_constant<int, 256>());
+    if (pieces <= 4 * 256 && K <= 256) return iters(std::integral_constant<int, 256>());
     return iters(std::integral_constant<int, 1024>());
 }
 
@@ -247,10 +245,10 @@ hipError_t distill(const DistillLogits& d, float* loss, float* lse, const float*
     a.scale = d.scale, a.rows = d.rows, a.V = d.V, a.K = d.K, a.tau = d.tau, a.to2 = kLog2e / d.tau;
     a.loss = loss, a.lse_out = lse, a.dloss = dloss, a.lse_in = lse;
     a.dlogits = static_cast<T*>(d.dlogits), a.ld_d = d.ld_d;
-    return with_shape<MODE, T>(d.V, [&](auto block, auto iter) {
+    return with_shape<MODE, T>(d.V, d.K, [&](auto block, auto iter) {
         constexpr int B = decltype(block)::value, ITER = decltype(iter)::value;
         hipLaunchKernelGGL((distill_kernel<T, B, ITER, MODE>),
-                           dim3(uint32_t(d.rows < kMaxBlocks ? d.rows : kMaxBlocks)), dim3(B), 0, stream, a);
+                           dim3(uint32_t(d.rows)), dim3(B), 0, stream, a);
         return hipGetLastError();
     });
 }

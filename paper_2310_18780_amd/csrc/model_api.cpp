@@ -115,7 +115,8 @@ lh_status check_distill_sizes(int64_t rows, int64_t V, int64_t K)
         return s;
     if (K < 1 || K > LH_DISTILL_MAX_TOP)
         return fail(LH_ERR_INVALID_ARG, "K = %lld must be in [1, %d]", (long long)K, LH_DISTILL_MAX_TOP);
-    return check_product("rows, V, K", rows, V, K);
+    if ((s = check_product("rows, V, K", rows, V, K))) return s;
+    return rows < (INT64_C(1) << 22) ? LH_OK : check_threads(rows * 1024);  // (a workgroup to a row)
 }
 
 // What both distillation calls take; ins gets 4 buffers.

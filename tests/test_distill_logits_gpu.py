@@ -172,7 +172,8 @@ def test_ids_given_twice_and_logits_of_minus_infinity(V):
     # a logit of minus infinity that the teacher asks for
     c["logits"][0, 5] = float("-inf")
     lh.distill_logits(loss=loss, dlogits=grad, **c)
-    assert loss[0] == float("inf") and grad[0, 5] == -1
+    # (the four slots' p are all: the same four numbers are added in two orders, three roundings each, and divided)
+    assert loss[0] == float("inf") and abs(grad[0, 5].item() + 1) <= 8 * U
     # NaN, on either side, is its row's alone
     c["logits"][0, 5] = 0
     c["logits"][1, 7], c["values"][4, 1] = float("nan"), float("nan")
