@@ -101,7 +101,16 @@ __global__ __launch_bounds__(BLOCK, ITER <= 8 ? 8 : 4) void distill_kernel(Args<
                 forget(raw[i]);
             }
         } else {
-            for (int p = threadIdx.x; p < pieces; p += BLOCK) f(load_raw<V>(x + int64_t(p) * V), p);
+            constexpr int kAhead = 4;  // pieces in flight
+            for (int p0 = threadIdx.x; p0 < pieces; p0 += kAhead * BLOCK) {
+                Raw<T, V> r[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    if (p0 + i * BLOCK < pieces) r[i] = load_raw<V>(x + int64_t(p0 + i * BLOCK) * V);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    if (p0 + i * BLOCK < pieces) f(r[i], p0 + i * BLOCK);
+            }
         }
     };
     if (scale != 0.f) {

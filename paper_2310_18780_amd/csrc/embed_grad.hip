@@ -5,11 +5,14 @@
 // same bits on every call.  Then a workgroup takes a window of sorted tokens and walks it with
 // its columns in registers: what begins and ends in the window is stored, what crosses a
 // border goes to the workspace (at most one run enters and one leaves a window), and a last
-// launch adds those, window by window.  Rows without a token are zeros, which further
-// workgroups of the first launch write while the sort runs.
+// launch adds those, window by window.
 //
-// Bound by memory: n rows of dy are read, V rows of dW written (those with tokens twice),
-// beside launches of a few microseconds each.
+// Rows without a token are zeros.  The sort's launches are short and leave the GPU idle, so each
+// has further workgroups that store their share of zeros to all of dW; rows with tokens
+// are stored again.
+//
+// Bound by memory: n rows of dy are read, V rows of dW written, beside launches of a few
+// microseconds each.
 #include "embed.hpp"
 
 #include "block_ops.hpp"
@@ -29,21 +32,24 @@ __device__ __forceinline__ uint32_t key_of(int id, uint32_t V)
     return uint32_t(id) < V ? uint32_t(id) : V;
 }
 
-// Zeros of dW by the workgroups from `first` on.
-__device__ __forceinline__ void fill_zeros(float* dW, int64_t count, int64_t first)
+// A launch's share of the zeros of dW (p = NULL: none), which the workgroups from `first` on store.
+struct Zeros {
+    float* p;
+    int64_t count;
+};
+__device__ __forceinline__ void store_zeros(const Zeros& z, int64_t first)
 {
-    if (!dW) return;
+    // whole pieces from the first 16-byte border on
+    const int64_t head0 = (16 - (reinterpret_cast<uintptr_t>(z.p) & 15)) / 4 & 3;
+    const int64_t head = head0 < z.count ? head0 : z.count;
+    const int64_t body = (z.count - head) / 4 * 4;
     const int64_t step = (int64_t(gridDim.x) - first) * blockDim.x * 4;
-    // (dW is a float's multiple; whole pieces from the first 16-byte border on)
-    const int64_t head0 = (16 - (reinterpret_cast<uintptr_t>(dW) & 15)) / 4 & 3;
-    const int64_t head = head0 < count ? head0 : count;
-    const int64_t body = (count - head) / 4 * 4;
-    const int64_t at = ((int64_t(blockIdx.x) - first) * blockDim.x + threadIdx.x) * 4;
-    float4* p = reinterpret_cast<float4*>(dW + head);
-    for (int64_t i = at; i < body; i += step) p[i / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4* p = reinterpret_cast<float4*>(z.p + head);
+    for (int64_t i = ((int64_t(blockIdx.x) - first) * blockDim.x + threadIdx.x) * 4; i < body; i += step)
+        p[i / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (int64_t(blockIdx.x) == first) {
-        if (threadIdx.x < head) dW[threadIdx.x] = 0.f;
-        if (head + body + threadIdx.x < count && threadIdx.x < 4) dW[head + body + threadIdx.x] = 0.f;
+        if (threadIdx.x < head) z.p[threadIdx.x] = 0.f;
+        if (threadIdx.x < z.count - head - body) z.p[head + body + threadIdx.x] = 0.f;
     }
 }
 
@@ -103,13 +109,13 @@ __device__ __forceinline__ void clear_counts(uint16_t (*counts)[kMaxDigits])
     __syncthreads();
 }
 
-// All tokens in one workgroup; the others fill dW.
+// All tokens in one workgroup.
 __global__ __launch_bounds__(kSortBlock) void sort_small_kernel(
     const int* __restrict__ ids, int n, uint32_t V, int passes, int bits, uint32_t* __restrict__ keys,
-    uint32_t* __restrict__ rows, float* dW, int64_t count)
+    uint32_t* __restrict__ rows, Zeros zeros)
 {
     if (blockIdx.x > 0) {
-        fill_zeros(dW, count, 1);
+        store_zeros(zeros, 1);
         return;
     }
     __shared__ uint32_t key[2][kSmall], row[2][kSmall];
@@ -151,15 +157,16 @@ __global__ __launch_bounds__(kSortBlock) void sort_small_kernel(
     }
 }
 
-// Tokens of each digit in each tile: counts [tiles, digits].  FIRST: the keys are the ids,
-// and the workgroups past the tiles fill dW.
+// Tokens of each value of a digit in each tile: counts [tiles, digits].  FIRST: the keys are the
+// ids.  (Counting the next digit where the one before is placed, by atomics on the tiles' counts,
+// takes 8 us more than this launch: a few values are most of them.)
 template <bool FIRST>
 __global__ __launch_bounds__(kSortBlock) void sort_count_kernel(
     const uint32_t* __restrict__ keys, int64_t n, uint32_t V, int shift, int bits, int64_t tile,
-    int64_t tiles, uint32_t* __restrict__ counts, float* dW, int64_t count)
+    int64_t tiles, uint32_t* __restrict__ counts, Zeros zeros)
 {
-    if (FIRST && int64_t(blockIdx.x) >= tiles) {
-        fill_zeros(dW, count, tiles);
+    if (int64_t(blockIdx.x) >= tiles) {
+        store_zeros(zeros, tiles);
         return;
     }
     __shared__ uint32_t total[kMaxDigits];
@@ -176,27 +183,34 @@ __global__ __launch_bounds__(kSortBlock) void sort_count_kernel(
         counts[blockIdx.x * int64_t(mask + 1) + d] = total[d];
 }
 
+// Places the tokens by one digit (FIRST: of the ids themselves).
 template <bool FIRST>
 __global__ __launch_bounds__(kSortBlock) void sort_place_kernel(
     const uint32_t* __restrict__ keys, const uint32_t* __restrict__ rows, int64_t n, uint32_t V,
     int shift, int bits, int64_t tile, int64_t tiles, const uint32_t* __restrict__ counts,
-    uint32_t* __restrict__ keys_out, uint32_t* __restrict__ rows_out)
+    uint32_t* __restrict__ keys_out, uint32_t* __restrict__ rows_out, Zeros zeros)
 {
+    if (int64_t(blockIdx.x) >= tiles) {
+        store_zeros(zeros, tiles);
+        return;
+    }
     __shared__ uint16_t in_wave[kSortWaves][kMaxDigits];
     __shared__ uint32_t totals[kMaxDigits], first[kMaxDigits], mine[kMaxDigits];
     const uint32_t mask = (1u << bits) - 1;
-    // a digit's first place in this tile: all tokens of lower digits, and its own in tiles before
-    for (int d = threadIdx.x; d <= int(mask); d += kSortBlock) {
-        uint32_t all = 0, before = 0;
+    // a digit's first place in this tile: all tokens of lower digits, and its own in tiles before;
+    // as many threads to a digit as there are
+    for (int d = threadIdx.x; d <= int(mask); d += kSortBlock) first[d] = mine[d] = 0;
+    __syncthreads();
+    const int d0 = threadIdx.x & int(mask), parts = kSortBlock >> bits;
+    uint32_t all = 0, before = 0;
 #pragma unroll 8
-        for (int64_t t = 0; t < tiles; ++t) {
-            const uint32_t c = counts[t * (mask + 1) + d];
-            before += t < int64_t(blockIdx.x) ? c : 0;
-            all += c;
-        }
-        first[d] = all;
-        mine[d] = before;
+    for (int64_t t = threadIdx.x >> bits; t < tiles; t += parts) {
+        const uint32_t c = counts[t * (mask + 1) + d0];
+        before += t < int64_t(blockIdx.x) ? c : 0;
+        all += c;
     }
+    atomicAdd(&first[d0], all);
+    atomicAdd(&mine[d0], before);
     __syncthreads();
     exclusive_sum(first, int(mask) + 1);
     for (int d = threadIdx.x; d <= int(mask); d += kSortBlock) first[d] += mine[d];
@@ -279,63 +293,84 @@ __global__ __launch_bounds__(kSumBlock) void runs_kernel(
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] = 0.f;
     };
+    // the rows of the next tokens are in flight while those before are added
     constexpr int kAhead = 8;
+    Raw<T, V> raw[kAhead], next[kAhead];
+    auto load = [&](Raw<T, V>(&r)[kAhead], int64_t p) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) r[i] = load_raw<V>(dy + int64_t(rows[p + i < p1 ? p + i : p1 - 1]) * D + c);
+    };
+    load(raw, p0);
     for (int64_t p = p0; p < p1; p += kAhead) {
-        Raw<T, V> raw[kAhead];
+        if (p + kAhead < p1) load(next, p + kAhead);
         uint32_t key[kAhead + 1];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int64_t q = p + i < p1 ? p + i : p1 - 1;
-            key[i] = keys[q];
-            raw[i] = load_raw<V>(dy + int64_t(rows[q]) * D + c);
-        }
-        key[kAhead] = p + kAhead < p1 ? keys[p + kAhead] : ~0u;
+        for (int i = 0; i <= kAhead; ++i) key[i] = keys[p + i < p1 ? p + i : p1 - 1];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (p + i >= p1 || key[i] >= rows_of_table) break;
+            if (p + i >= p1 || key[i] >= rows_of_table) return;
             float v[V];
             expand<V, T>(raw[i], v);
 #pragma unroll
             for (int j = 0; j < V; ++j) acc[j] += v[j];
             if (p + i + 1 == p1 || key[i + 1] != key[i]) close(p + i, key[i]);
         }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) raw[i] = next[i];
     }
 }
 
 // Runs that cross windows, each by the workgroups of the window that it begins in.
+template <int V>
 __global__ __launch_bounds__(kSumBlock) void joins_kernel(
     const uint32_t* __restrict__ keys, int64_t n, uint32_t rows_of_table, int64_t D, int window,
     float scale, bool accumulate, float* __restrict__ dW, const float* __restrict__ part)
 {
-    const int64_t blocks = (D + kSumBlock - 1) / kSumBlock;
+    const int64_t blocks = (D + kSumBlock * V - 1) / (kSumBlock * V);
     const int64_t w = blockIdx.x / blocks;
-    const int64_t c = blockIdx.x % blocks * kSumBlock + threadIdx.x;
+    const int64_t c0 = (blockIdx.x % blocks * kSumBlock + threadIdx.x) * V;
     const int64_t p0 = w * window, p1 = p0 + window;
     if (p1 >= n) return;
     const uint32_t key = keys[p1 - 1];
     if (key >= rows_of_table || keys[p1] != key) return;          // nothing leaves
     if (keys[p0] == key && p0 > 0 && keys[p0 - 1] == key) return;  // it began before
-    if (c >= D) return;
-    // the last window that the run reaches: its first token is of the run
+    if (c0 >= D) return;
+    const int64_t c = c0 + V <= D ? c0 : D - V;
+    auto get = [&](int64_t slot, float(&v)[V]) { expand<V, float>(load_raw<V>(part + slot * D + c), v); };
+    float acc[V];
+    get(w * 2 + 1, acc);
+    // the windows that the run reaches: their first token is of the run
+    constexpr int kAhead = 8;
     const int64_t windows = (n + window - 1) / window;
-    int64_t last = w + 1, hi = windows - 1;
-    while (last < hi) {
-        const int64_t mid = (last + hi + 1) / 2;
-        if (keys[mid * window] == key) last = mid;
-        else hi = mid - 1;
-    }
-    float acc = part[(w * 2 + 1) * D + c];
-    int64_t j = w + 1;
-    for (; j + 7 <= last; j += 8) {
-        float v[8];
+    bool more = true;
+    for (int64_t j = w + 1; more && j < windows; j += kAhead) {
+        float v[kAhead][V];
+        uint32_t k[kAhead];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = part[(j + i) * 2 * D + c];
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t at = j + i < windows ? j + i : windows - 1;
+            k[i] = keys[at * window];
+            get(at * 2, v[i]);
+        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc += v[i];
+        for (int i = 0; i < kAhead; ++i) {
+            more = more && j + i < windows && k[i] == key;
+            if (more) {
+#pragma unroll
+                for (int l = 0; l < V; ++l) acc[l] += v[i][l];
+            }
+        }
     }
-    for (; j <= last; ++j) acc += part[j * 2 * D + c];
     float* out = dW + int64_t(key) * D + c;
-    *out = accumulate ? *out + acc * scale : acc * scale;
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[k] *= scale;
+    if (accumulate) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (k >= int(c0 - c)) out[k] += acc[k];
+    } else {
+        put_sums<V>(out, acc);
+    }
 }
 
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
@@ -345,16 +380,18 @@ hipError_t launch_runs(const T* dy, const uint32_t* keys, const uint32_t* rows, 
                        int64_t D, const EmbedGradPlan& p, float scale, bool accumulate, float* dW,
                        float* part, hipStream_t stream)
 {
-    constexpr int kV = kVec<T>;
-    const int v = D < kV ? 1 : kV;
-    const dim3 grid(uint32_t(p.windows * ((D + kSumBlock * v - 1) / (kSumBlock * v))));
-    if (v == 1)
-        hipLaunchKernelGGL((runs_kernel<T, 1>), grid, dim3(kSumBlock), 0, stream, dy, keys, rows, n,
-                           uint32_t(V), D, int(p.window), scale, accumulate, dW, part);
-    else
-        hipLaunchKernelGGL((runs_kernel<T, kV>), grid, dim3(kSumBlock), 0, stream, dy, keys, rows, n,
-                           uint32_t(V), D, int(p.window), scale, accumulate, dW, part);
-    return hipGetLastError();
+    auto launch = [&](auto wide) {
+        constexpr int v = decltype(wide)::value;
+        const int64_t blocks = p.windows * ((D + kSumBlock * v - 1) / (kSumBlock * v));
+        hipLaunchKernelGGL((runs_kernel<T, v>), dim3(uint32_t(blocks)), dim3(kSumBlock), 0, stream, dy, keys,
+                           rows, n, uint32_t(V), D, int(p.window), scale, accumulate, dW, part);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        hipLaunchKernelGGL((joins_kernel<v>), dim3(uint32_t(blocks)), dim3(kSumBlock), 0, stream, keys, n, uint32_t(V), D, int(p.window), scale, accumulate, dW,
+                           part);
+        return hipGetLastError();
+    };
+    if (D < 4) return launch(std::integral_constant<int, 1>());
+    return launch(std::integral_constant<int, 4>());
 }
 
 }  // namespace
@@ -401,51 +438,55 @@ hipError_t launch_embed_grad(const void* dy, const int32_t* ids, int64_t n, int6
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + p.off_keys[0]), reinterpret_cast<uint32_t*>(ws + p.off_keys[1])};
     uint32_t* rows[2] = {reinterpret_cast<uint32_t*>(ws + p.off_rows[0]), reinterpret_cast<uint32_t*>(ws + p.off_rows[1])};
     float* part = reinterpret_cast<float*>(ws + p.off_part);
-    float* fill = accumulate ? nullptr : dW;
-    const int64_t count = V * D;
-    // workgroups that fill: 16 KiB each at least
-    int64_t fills = fill ? (count + 4095) / 4096 : 0;
-    fills = fills < kFillBlocks ? fills : kFillBlocks;
     hipError_t e;
     int at = 0;  // where the sorted tokens are
+    // each sorting launch's share of the zeros, 16 KiB to a workgroup at least
+    const int launches = p.tiles > 0 ? 2 * p.passes : 1;
+    int launch = 0;
+    auto share = [&] {
+        const int64_t all = accumulate ? 0 : V * D, i = launch++;
+        const int64_t from = all / launches * i, to = i + 1 < launches ? all / launches * (i + 1) : all;
+        return Zeros{dW + from, to - from};
+    };
+    auto grid = [](int64_t sorting, const Zeros& z) {
+        const int64_t n = (z.count + 4095) / 4096;
+        return dim3(uint32_t(sorting + (n < kFillBlocks ? n : kFillBlocks)));
+    };
+    const dim3 block(kSortBlock);
     if (p.tiles == 0) {
-        if (n == 0 && fills == 0) return hipSuccess;
-        hipLaunchKernelGGL(sort_small_kernel, dim3(uint32_t(1 + fills)), dim3(kSortBlock), 0, stream, ids,
-                           int(n), uint32_t(V), p.passes, p.bits, keys[0], rows[0], fill, count);
+        const Zeros z = share();
+        if (n == 0 && z.count == 0) return hipSuccess;
+        hipLaunchKernelGGL(sort_small_kernel, grid(1, z), block, 0, stream, ids, int(n), uint32_t(V), p.passes, p.bits,
+                           keys[0], rows[0], z);
         if ((e = hipGetLastError()) != hipSuccess || n == 0) return e;
     } else {
         uint32_t* counts = reinterpret_cast<uint32_t*>(ws + p.off_counts);
-        const dim3 grid(uint32_t(p.tiles)), block(kSortBlock);
         for (int i = 0; i < p.passes; ++i) {
-            const int shift = i * p.bits;
+            const int to = i & 1, shift = i * p.bits;
+            const Zeros z0 = share(), z1 = share();
             if (i == 0) {
                 const uint32_t* in = reinterpret_cast<const uint32_t*>(ids);
-                hipLaunchKernelGGL((sort_count_kernel<true>), dim3(uint32_t(p.tiles + fills)), block, 0, stream,
-                                   in, n, uint32_t(V), shift, p.bits, p.tile, p.tiles, counts, fill, count);
+                hipLaunchKernelGGL((sort_count_kernel<true>), grid(p.tiles, z0), block, 0, stream, in, n, uint32_t(V),
+                                   shift, p.bits, p.tile, p.tiles, counts, z0);
                 if ((e = hipGetLastError()) != hipSuccess) return e;
-                hipLaunchKernelGGL((sort_place_kernel<true>), grid, block, 0, stream, in,
+                hipLaunchKernelGGL((sort_place_kernel<true>), grid(p.tiles, z1), block, 0, stream, in,
                                    static_cast<const uint32_t*>(nullptr), n, uint32_t(V), shift, p.bits, p.tile,
-                                   p.tiles, counts, keys[0], rows[0]);
+                                   p.tiles, counts, keys[to], rows[to], z1);
             } else {
-                hipLaunchKernelGGL((sort_count_kernel<false>), grid, block, 0, stream, keys[at], n, uint32_t(V),
-                                   shift, p.bits, p.tile, p.tiles, counts, static_cast<float*>(nullptr), int64_t(0));
+                hipLaunchKernelGGL((sort_count_kernel<false>), grid(p.tiles, z0), block, 0, stream, keys[at], n,
+                                   uint32_t(V), shift, p.bits, p.tile, p.tiles, counts, z0);
                 if ((e = hipGetLastError()) != hipSuccess) return e;
-                hipLaunchKernelGGL((sort_place_kernel<false>), grid, block, 0, stream, keys[at], rows[at], n,
-                                   uint32_t(V), shift, p.bits, p.tile, p.tiles, counts, keys[at ^ 1], rows[at ^ 1]);
-                at ^= 1;
+                hipLaunchKernelGGL((sort_place_kernel<false>), grid(p.tiles, z1), block, 0, stream, keys[at], rows[at],
+                                   n, uint32_t(V), shift, p.bits, p.tile, p.tiles, counts, keys[to], rows[to], z1);
             }
             if ((e = hipGetLastError()) != hipSuccess) return e;
+            at = to;
         }
     }
-    e = bf16_io ? launch_runs(static_cast<const bf16*>(dy), keys[at], rows[at], n, V, D, p, scale, accumulate,
-                              dW, part, stream)
-                : launch_runs(static_cast<const float*>(dy), keys[at], rows[at], n, V, D, p, scale, accumulate,
-                              dW, part, stream);
-    if (e != hipSuccess) return e;
-    const int64_t blocks = (D + kSumBlock - 1) / kSumBlock;
-    hipLaunchKernelGGL(joins_kernel, dim3(uint32_t(p.windows * blocks)), dim3(kSumBlock), 0, stream, keys[at], n,
-                       uint32_t(V), D, int(p.window), scale, accumulate, dW, part);
-    return hipGetLastError();
+    return bf16_io ? launch_runs(static_cast<const bf16*>(dy), keys[at], rows[at], n, V, D, p, scale, accumulate,
+                                 dW, part, stream)
+                   : launch_runs(static_cast<const float*>(dy), keys[at], rows[at], n, V, D, p, scale, accumulate,
+                                 dW, part, stream);
 }
 
 }  // namespace lh
