@@ -261,19 +261,25 @@ __global__ __launch_bounds__(kSumBlock) void runs_kernel(
 {
     const int64_t blocks = (D + kSumBlock * V - 1) / (kSumBlock * V);
     const int64_t w = blockIdx.x / blocks;
+    // (A piece that would pass the row's end starts before it, one past it repeats the last: lanes
+    // store the same bits to the same place, but where they add to what is there, which only the
+    // lane that owns a value may.  No lane ends early: the window's ids lie in all of them.)
     const int64_t c0 = (blockIdx.x % blocks * kSumBlock + threadIdx.x) * V;
-    if (c0 >= D) return;
-    // (a piece that would pass the row's end starts before it: two lanes store the same bits,
-    // but where they add to what is there, which only the one that owns a value may)
     const int64_t c = c0 + V <= D ? c0 : D - V;
-    const int twice = int(c0 - c);
+    const int twice = int(c0 - c < V ? c0 - c : V);
     const int64_t p0 = w * window, p1 = p0 + window < n ? p0 + window : n;
+    // The window's ids and rows lie in the lanes of each wavefront (a window is 64 tokens or
+    // fewer): loaded one by one as scalars, each would be waited for before the next is asked for
+    // (129 us at 65536 x 2048 bfloat16).
+    const int64_t mine = p0 + threadIdx.x % kWave < p1 ? p0 + threadIdx.x % kWave : p1 - 1;
+    const int my_key = int(keys[mine]), my_row = int(rows[mine]);
+    auto key_at = [&](int q) { return uint32_t(__builtin_amdgcn_readlane(my_key, q)); };
     const uint32_t entered = p0 > 0 ? keys[p0 - 1] : ~0u, leaves = p1 < n ? keys[p1] : ~0u;
-    if (keys[p0] >= rows_of_table) return;
-    bool in_run = keys[p0] == entered;  // of a token before the window
+    if (key_at(0) >= rows_of_table) return;
+    bool in_run = key_at(0) == entered;  // of a token before the window
     float acc[V] = {};
-    auto close = [&](int64_t p, uint32_t key) {  // the run that ends with token p
-        if (p + 1 == p1 && key == leaves) {
+    auto close = [&](int q, uint32_t key) {  // the run that ends with token q of the window
+        if (p0 + q + 1 == p1 && key == leaves) {
             put_sums<V>(part + (w * 2 + (in_run ? 0 : 1)) * D + c, acc);
         } else if (in_run) {
             put_sums<V>(part + w * 2 * D + c, acc);
@@ -295,28 +301,35 @@ __global__ __launch_bounds__(kSumBlock) void runs_kernel(
     };
     // the rows of the next tokens are in flight while those before are added
     constexpr int kAhead = 8;
-    Raw<T, V> raw[kAhead], next[kAhead];
-    auto load = [&](Raw<T, V>(&r)[kAhead], int64_t p) {
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) r[i] = load_raw<V>(dy + int64_t(rows[p + i < p1 ? p + i : p1 - 1]) * D + c);
-    };
-    load(raw, p0);
-    for (int64_t p = p0; p < p1; p += kAhead) {
-        if (p + kAhead < p1) load(next, p + kAhead);
-        uint32_t key[kAhead + 1];
-#pragma unroll
-        for (int i = 0; i <= kAhead; ++i) key[i] = keys[p + i < p1 ? p + i : p1 - 1];
+    const int tokens = int(p1 - p0);
+    Raw<T, V> raw[kAhead];
+    auto load = [&](int q) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (p + i >= p1 || key[i] >= rows_of_table) return;
-            float v[V];
-            expand<V, T>(raw[i], v);
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += v[j];
-            if (p + i + 1 == p1 || key[i + 1] != key[i]) close(p + i, key[i]);
+            const uint32_t row = uint32_t(__builtin_amdgcn_readlane(my_row, q + i < tokens ? q + i : tokens - 1));
+            raw[i] = load_raw<V>(dy + int64_t(row) * D + c);
         }
+    };
+    load(0);
+    for (int q = 0; q < tokens; q += kAhead) {
+        float v[kAhead][V];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) raw[i] = next[i];
+        for (int i = 0; i < kAhead; ++i) {
+            expand<V, T>(raw[i], v[i]);
+            // (waited for here: past a store, a wait for them would be one for the store too)
+#pragma unroll
+            for (int j = 0; j < V; ++j) asm volatile("" : "+v"(v[i][j]));
+        }
+        if (q + kAhead < tokens) load(q + kAhead);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (q + i >= tokens) return;
+            const uint32_t key = key_at(q + i);
+            if (key >= rows_of_table) return;
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] += v[i][j];
+            if (q + i + 1 == tokens || key_at(q + i + 1) != key) close(q + i, key);
+        }
     }
 }
 
@@ -399,7 +412,7 @@ hipError_t launch_runs(const T* dy, const uint32_t* keys, const uint32_t* rows, 
 EmbedGradPlan embed_grad_plan(int64_t n, int64_t V, int64_t D)
 {
     EmbedGradPlan p{};
-    p.window = n <= 8192 ? 16 : 64;
+    p.window = n <= 8192 ? 16 : kWave;
     p.windows = (n + p.window - 1) / p.window;
     int bits = 1;  // of the keys 0 .. V
     while (V >> bits) ++bits;
