@@ -11,8 +11,13 @@
 // has further workgroups that store their share of zeros to all of dW; rows with tokens
 // are stored again.
 //
-// Bound by memory: n rows of dy are read, V rows of dW written, beside launches of a few
-// microseconds each.
+// Bound by memory: n rows of dy are read, V rows of dW written and the rows with tokens once
+// more, beside launches of a few microseconds each.  65536 tokens of bfloat16 x 2048 with a
+// table of 50000 rows, 16600 of them met: 66 us the sort and the zeros (6.2 TB/s), 125 the runs,
+// 12 the joins.  Other ways that were built for the zeros: a fill of its own before the sort,
+// 228 us in all against 203; only the rows without a token, which the sums' launch looks up
+// among the sorted keys, 196, with a search in every row of it; the same from a bit per row that
+// the sort sets, 344 (many tokens of few rows meet in an atomic).
 #include "embed.hpp"
 
 #include "block_ops.hpp"
@@ -24,7 +29,7 @@ constexpr int kSortBlock = 1024;
 constexpr int kSortWaves = kSortBlock / kWave;
 constexpr int kMaxBits = 9, kMaxDigits = 1 << kMaxBits;
 constexpr int64_t kSmall = 4096;  // tokens that one workgroup sorts in LDS
-constexpr int kFillBlocks = 2048;
+constexpr int kFillBlocks = 2048;  // workgroups that store zeros beside a launch's own, at most
 
 // The sort key of an id: ids outside the table come last and take no part.
 __device__ __forceinline__ uint32_t key_of(int id, uint32_t V)
@@ -269,31 +274,32 @@ __global__ __launch_bounds__(kSumBlock) void runs_kernel(
     const int twice = int(c0 - c < V ? c0 - c : V);
     const int64_t p0 = w * window, p1 = p0 + window < n ? p0 + window : n;
     // The window's ids and rows lie in the lanes of each wavefront (a window is 64 tokens or
-    // fewer): loaded one by one as scalars, each would be waited for before the next is asked for
-    // (129 us at 65536 x 2048 bfloat16).
-    const int64_t mine = p0 + threadIdx.x % kWave < p1 ? p0 + threadIdx.x % kWave : p1 - 1;
-    const int my_key = int(keys[mine]), my_row = int(rows[mine]);
-    auto key_at = [&](int q) { return uint32_t(__builtin_amdgcn_readlane(my_key, q)); };
+    // fewer): loaded one by one as scalars, each would be waited for before the next is asked for.
+    // The tokens that take part come first; where runs end is a bit for each token.
+    const int lane = threadIdx.x % kWave, tokens = int(p1 - p0);
+    const int64_t mine = lane < tokens ? p0 + lane : p1 - 1;
+    const uint32_t my_key = keys[mine], my_row = rows[mine];
     const uint32_t entered = p0 > 0 ? keys[p0 - 1] : ~0u, leaves = p1 < n ? keys[p1] : ~0u;
-    if (key_at(0) >= rows_of_table) return;
-    bool in_run = key_at(0) == entered;  // of a token before the window
+    const int valid = __popcll(__ballot(lane < tokens && my_key < rows_of_table));
+    if (valid == 0) return;
+    const uint32_t next_key = __shfl_down(my_key, 1, kWave);
+    const uint64_t ends = __ballot(lane < valid && (lane + 1 == valid || next_key != my_key));
+    bool in_run = uint32_t(__builtin_amdgcn_readlane(int(my_key), 0)) == entered;  // of a token before the window
     float acc[V] = {};
-    auto close = [&](int q, uint32_t key) {  // the run that ends with token q of the window
-        if (p0 + q + 1 == p1 && key == leaves) {
-            put_sums<V>(part + (w * 2 + (in_run ? 0 : 1)) * D + c, acc);
-        } else if (in_run) {
-            put_sums<V>(part + w * 2 * D + c, acc);
+    auto close = [&](int q) {  // the run that ends with token q
+        const uint32_t key = uint32_t(__builtin_amdgcn_readlane(int(my_key), q));
+        const bool leaving = q + 1 == tokens && key == leaves, partial = in_run || leaving;
+        float* out = partial ? part + (w * 2 + (in_run ? 0 : 1)) * D + c : dW + int64_t(key) * D + c;
+        const float factor = partial ? 1.f : scale;
+        if (accumulate && !partial) {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (j >= twice) out[j] += acc[j] * factor;
         } else {
-            float* out = dW + int64_t(key) * D + c;
+            float sum[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] *= scale;
-            if (accumulate) {
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (j >= twice) out[j] += acc[j];
-            } else {
-                put_sums<V>(out, acc);
-            }
+            for (int j = 0; j < V; ++j) sum[j] = acc[j] * factor;
+            put_sums<V>(out, sum);
         }
         in_run = false;
 #pragma unroll
@@ -301,17 +307,16 @@ __global__ __launch_bounds__(kSumBlock) void runs_kernel(
     };
     // the rows of the next tokens are in flight while those before are added
     constexpr int kAhead = 8;
-    const int tokens = int(p1 - p0);
     Raw<T, V> raw[kAhead];
     auto load = [&](int q) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const uint32_t row = uint32_t(__builtin_amdgcn_readlane(my_row, q + i < tokens ? q + i : tokens - 1));
+            const uint32_t row = uint32_t(__builtin_amdgcn_readlane(int(my_row), q + i < valid ? q + i : valid - 1));
             raw[i] = load_raw<V>(dy + int64_t(row) * D + c);
         }
     };
     load(0);
-    for (int q = 0; q < tokens; q += kAhead) {
+    for (int q = 0; q < valid; q += kAhead) {
         float v[kAhead][V];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -320,63 +325,80 @@ __global__ __launch_bounds__(kSumBlock) void runs_kernel(
 #pragma unroll
             for (int j = 0; j < V; ++j) asm volatile("" : "+v"(v[i][j]));
         }
-        if (q + kAhead < tokens) load(q + kAhead);
+        if (q + kAhead < valid) load(q + kAhead);
+        const uint32_t here = uint32_t(ends >> q) & ((1u << kAhead) - 1);
+        if (here == 0) {  // in the middle of a run
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (q + i >= tokens) return;
-            const uint32_t key = key_at(q + i);
-            if (key >= rows_of_table) return;
+            for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += v[i][j];
-            if (q + i + 1 == tokens || key_at(q + i + 1) != key) close(q + i, key);
+                for (int j = 0; j < V; ++j) acc[j] += v[i][j];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (q + i >= valid) return;
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] += v[i][j];
+                if (here >> i & 1) close(q + i);
+            }
         }
     }
 }
 
-// Runs that cross windows, each by the workgroups of the window that it begins in.
+// Runs that cross windows, each by the workgroups of the window that it begins in.  The lanes
+// count the windows that it reaches (their first tokens are of the run), and four wavefronts
+// to the same columns take them in turn: the longest run of a batch is one of many windows.
+constexpr int kJoinParts = 4;
+
 template <int V>
-__global__ __launch_bounds__(kSumBlock) void joins_kernel(
+__global__ __launch_bounds__(kSumBlock * kJoinParts) void joins_kernel(
     const uint32_t* __restrict__ keys, int64_t n, uint32_t rows_of_table, int64_t D, int window,
     float scale, bool accumulate, float* __restrict__ dW, const float* __restrict__ part)
 {
+    __shared__ float red[kJoinParts - 1][V][kSumBlock];
     const int64_t blocks = (D + kSumBlock * V - 1) / (kSumBlock * V);
     const int64_t w = blockIdx.x / blocks;
-    const int64_t c0 = (blockIdx.x % blocks * kSumBlock + threadIdx.x) * V;
+    const int column = threadIdx.x % kSumBlock, turn = threadIdx.x / kSumBlock, lane = threadIdx.x % kWave;
     const int64_t p0 = w * window, p1 = p0 + window;
     if (p1 >= n) return;
     const uint32_t key = keys[p1 - 1];
-    if (key >= rows_of_table || keys[p1] != key) return;          // nothing leaves
+    if (key >= rows_of_table || keys[p1] != key) return;           // nothing leaves
     if (keys[p0] == key && p0 > 0 && keys[p0 - 1] == key) return;  // it began before
-    if (c0 >= D) return;
+    const int64_t c0 = (blockIdx.x % blocks * kSumBlock + column) * V;
     const int64_t c = c0 + V <= D ? c0 : D - V;
     auto get = [&](int64_t slot, float(&v)[V]) { expand<V, float>(load_raw<V>(part + slot * D + c), v); };
-    float acc[V];
-    get(w * 2 + 1, acc);
-    // the windows that the run reaches: their first token is of the run
-    constexpr int kAhead = 8;
     const int64_t windows = (n + window - 1) / window;
-    bool more = true;
-    for (int64_t j = w + 1; more && j < windows; j += kAhead) {
+    int64_t end = w + 1;
+    for (uint64_t more = ~uint64_t(0); more == ~uint64_t(0);) {
+        more = __ballot(end + lane < windows && keys[(end + lane) * window] == key);
+        end += more == ~uint64_t(0) ? kWave : __builtin_ctzll(~more);
+    }
+    float acc[V] = {};
+    if (turn == 0) get(w * 2 + 1, acc);
+    constexpr int kAhead = 8;
+    for (int64_t j = w + 1 + turn; j < end; j += kJoinParts * kAhead) {
         float v[kAhead][V];
-        uint32_t k[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int64_t at = j + i < windows ? j + i : windows - 1;
-            k[i] = keys[at * window];
-            get(at * 2, v[i]);
-        }
+        for (int i = 0; i < kAhead; ++i)
+            get((j + i * kJoinParts < end ? j + i * kJoinParts : j) * 2, v[i]);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            more = more && j + i < windows && k[i] == key;
-            if (more) {
+        for (int i = 0; i < kAhead; ++i)
+            if (j + i * kJoinParts < end) {
 #pragma unroll
                 for (int l = 0; l < V; ++l) acc[l] += v[i][l];
             }
-        }
+    }
+    if (turn > 0) {
+#pragma unroll
+        for (int l = 0; l < V; ++l) red[turn - 1][l][column] = acc[l];
+    }
+    __syncthreads();
+    if (turn > 0 || c0 >= D) return;
+#pragma unroll
+    for (int l = 0; l < V; ++l) {
+        for (int i = 0; i < kJoinParts - 1; ++i) acc[l] += red[i][l][column];
+        acc[l] *= scale;
     }
     float* out = dW + int64_t(key) * D + c;
-#pragma unroll
-    for (int k = 0; k < V; ++k) acc[k] *= scale;
     if (accumulate) {
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -396,11 +418,11 @@ hipError_t launch_runs(const T* dy, const uint32_t* keys, const uint32_t* rows, 
     auto launch = [&](auto wide) {
         constexpr int v = decltype(wide)::value;
         const int64_t blocks = p.windows * ((D + kSumBlock * v - 1) / (kSumBlock * v));
-        hipLaunchKernelGGL((runs_kernel<T, v>), dim3(uint32_t(blocks)), dim3(kSumBlock), 0, stream, dy, keys,
-                           rows, n, uint32_t(V), D, int(p.window), scale, accumulate, dW, part);
+        hipLaunchKernelGGL((runs_kernel<T, v>), dim3(uint32_t(blocks)), dim3(kSumBlock), 0, stream, dy, keys, rows, n,
+                           uint32_t(V), D, int(p.window), scale, accumulate, dW, part);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        hipLaunchKernelGGL((joins_kernel<v>), dim3(uint32_t(blocks)), dim3(kSumBlock), 0, stream, keys, n, uint32_t(V), D, int(p.window), scale, accumulate, dW,
-                           part);
+        hipLaunchKernelGGL((joins_kernel<v>), dim3(uint32_t(blocks)), dim3(kSumBlock * kJoinParts), 0, stream, keys, n, uint32_t(V),
+                           D, int(p.window), scale, accumulate, dW, part);
         return hipGetLastError();
     };
     if (D < 4) return launch(std::integral_constant<int, 1>());
@@ -412,6 +434,9 @@ hipError_t launch_runs(const T* dy, const uint32_t* keys, const uint32_t* rows, 
 EmbedGradPlan embed_grad_plan(int64_t n, int64_t V, int64_t D)
 {
     EmbedGradPlan p{};
+    // 64 tokens, one to a lane, where that gives windows enough for every CU; of few tokens 16, so
+    // that more workgroups share them (65536 tokens x 2048: runs and joins 124 + 13 us with windows
+    // of 64, 120 + 27 with 32, 120 + 46 with 16)
     p.window = n <= 8192 ? 16 : kWave;
     p.windows = (n + p.window - 1) / p.window;
     int bits = 1;  // of the keys 0 .. V
@@ -437,7 +462,8 @@ EmbedGradPlan embed_grad_plan(int64_t n, int64_t V, int64_t D)
 int64_t embed_grad_threads(int64_t n, int64_t V, int64_t D)
 {
     const EmbedGradPlan p = embed_grad_plan(n, V, D);
-    const int64_t sum = p.windows * ((D + kSumBlock - 1) / kSumBlock) * kSumBlock;
+    const int64_t columns = kSumBlock * (D < 4 ? 1 : 4);
+    const int64_t sum = p.windows * ((D + columns - 1) / columns) * kSumBlock * kJoinParts;
     const int64_t sort = (p.tiles + 1 + kFillBlocks) * kSortBlock;
     return sum > sort ? sum : sort;
 }

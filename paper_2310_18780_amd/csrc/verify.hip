@@ -142,13 +142,17 @@ __global__ __launch_bounds__(kBlock) void verify_pick_kernel(Rows<T> a, const do
     __shared__ double base;
     __shared__ int pick, latest;
     const int64_t b = blockIdx.x;
+    // (all that does not depend on the border is asked for at once)
     const int n = draft_length(a, b), m = a.accepted[b];
+    const float u_last = a.u_last[b];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int mine_drafted = threadIdx.x < a.K ? a.drafted[b * a.K + threadIdx.x] : -1;
+    const double2 first = wave == 0 && lane < a.tiles ? sums[b * a.tiles + lane] : make_double2(0., 0.);
     // the first wavefront adds the tiles' sums in order, 64 at a time, twice: the total, then the
     // tile whose end is past the border (or the last one with any weight)
     if (wave == 0) {
-        double2 all = make_double2(0., 0.);
-        for (int64_t i = lane; i < a.tiles; i += kWave) {
+        double2 all = first;
+        for (int64_t i = lane + kWave; i < a.tiles; i += kWave) {
             const double2 s = sums[b * a.tiles + i];
             all.x += s.x;
             all.y += s.y;
@@ -156,14 +160,14 @@ __global__ __launch_bounds__(kBlock) void verify_pick_kernel(Rows<T> a, const do
         all.x = wave_sum64(all.x);
         all.y = wave_sum64(all.y);
         const bool rest = all.x > 0.;
-        const double border = double(a.u_last[b]) * (rest ? all.x : all.y);
+        const double border = double(u_last) * (rest ? all.x : all.y);
         double before = 0., at = 0.;
         int64_t tile = -1, some = -1;
         double some_at = 0.;
         for (int64_t i0 = 0; i0 < a.tiles && tile < 0; i0 += kWave) {
             double x = 0.;
             if (i0 + lane < a.tiles) {
-                const double2 s = sums[b * a.tiles + i0 + lane];
+                const double2 s = i0 == 0 ? first : sums[b * a.tiles + i0 + lane];
                 x = rest ? s.x : s.y;
             }
             double c = x;
@@ -233,8 +237,8 @@ __global__ __launch_bounds__(kBlock) void verify_pick_kernel(Rows<T> a, const do
         __syncthreads();
     }
     const int next = pick >= 0 ? pick : latest;
-    for (int i = threadIdx.x; i <= a.K; i += kBlock)
-        a.tokens[b * (a.K + 1) + i] = i < m ? a.drafted[b * a.K + i] : i == m ? next : -1;
+    static_assert(LH_VERIFY_MAX_DRAFT < kBlock, "a thread for each token of a row");
+    if (const int i = threadIdx.x; i <= a.K) a.tokens[b * (a.K + 1) + i] = i < m ? mine_drafted : i == m ? next : -1;
 }
 
 int64_t tiles_of(int64_t V) { return (V + kTileV - 1) / kTileV; }
