@@ -12,7 +12,7 @@ hipError_t launch_embed(const void* W, const int32_t* ids, int64_t n, int64_t V,
 struct EmbedGradPlan {
     int64_t window;   // sorted tokens of a workgroup
     int64_t windows;
-    int64_t tile;     // tokens of a workgroup of the sort (0: one workgroup sorts all)
+    int64_t tile;     // tokens of a workgroup of the sort (0: few, that one launch places)
     int64_t tiles;
     int passes, bits;  // digits of the ids, and their bits
     size_t off_keys[2], off_rows[2], off_counts, off_part;

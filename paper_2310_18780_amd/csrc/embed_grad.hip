@@ -1,7 +1,7 @@
 // Gradient of the embedding's table: dW[v] = scale sum over the tokens k of id v of dy[k].
 //
-// The tokens are sorted by id (a stable counting sort, digit by digit, from the least), so
-// that a row's tokens lie side by side in the order of their positions and their sum has the
+// The tokens are sorted by id (a stable counting sort, digit by digit, from the least; few
+// tokens by counting for each what comes before it), so that a row's tokens lie side by side in the order of their positions and their sum has the
 // same bits on every call.  Then a workgroup takes a window of sorted tokens and walks it with
 // its columns in registers: what begins and ends in the window is stored, what crosses a
 // border goes to the workspace (at most one run enters and one leaves a window), and a last
@@ -28,7 +28,7 @@ namespace {
 constexpr int kSortBlock = 1024;
 constexpr int kSortWaves = kSortBlock / kWave;
 constexpr int kMaxBits = 9, kMaxDigits = 1 << kMaxBits;
-constexpr int64_t kSmall = 4096;  // tokens that one workgroup sorts in LDS
+constexpr int kSmall = 8192;  // tokens that are placed by counting, all keys in LDS
 constexpr int kFillBlocks = 2048;  // workgroups that store zeros beside a launch's own, at most
 
 // The sort key of an id: ids outside the table come last and take no part.
@@ -114,52 +114,57 @@ __device__ __forceinline__ void clear_counts(uint16_t (*counts)[kMaxDigits])
     __syncthreads();
 }
 
-// All tokens in one workgroup.
-__global__ __launch_bounds__(kSortBlock) void sort_small_kernel(
-    const int* __restrict__ ids, int n, uint32_t V, int passes, int bits, uint32_t* __restrict__ keys,
-    uint32_t* __restrict__ rows, Zeros zeros)
+// Few tokens in one launch: a token's place is the number of tokens that come before it, those of
+// lower keys and those of its own at lower positions.  Each wavefront counts for two tokens, over
+// all keys in LDS: a compare with a scalar and a count of its bits, 64 keys at a time.
+constexpr int kRankEach = 2, kRankTokens = kSortWaves * kRankEach;
+
+__global__ __launch_bounds__(kSortBlock) void rank_kernel(const int* __restrict__ ids, int n, uint32_t V,
+                                                          uint32_t* __restrict__ keys, uint32_t* __restrict__ rows,
+                                                          Zeros zeros)
 {
-    if (blockIdx.x > 0) {
-        store_zeros(zeros, 1);
+    const int own = (n + kRankTokens - 1) / kRankTokens;
+    if (int(blockIdx.x) >= own) {
+        store_zeros(zeros, own);
         return;
     }
-    __shared__ uint32_t key[2][kSmall], row[2][kSmall];
-    __shared__ uint16_t counts[kSortWaves][kMaxDigits];
-    __shared__ uint32_t totals[kMaxDigits], first[kMaxDigits];
-    for (int i = threadIdx.x; i < n; i += kSortBlock) {
-        key[0][i] = key_of(ids[i], V);
-        row[0][i] = i;
-    }
+    __shared__ __align__(16) uint32_t key[kSmall];
+    constexpr int kChunk = kWave * 4;  // keys of a wavefront's load
+    const int chunks = (n + kChunk - 1) / kChunk;
+    for (int i = threadIdx.x; i < chunks * kChunk; i += kSortBlock) key[i] = i < n ? key_of(ids[i], V) : ~0u;
     __syncthreads();
-    const uint32_t mask = (1u << bits) - 1;
-    for (int p = 0; p < passes; ++p) {
-        const uint32_t *k = key[p & 1], *r = row[p & 1];
-        uint32_t *ko = key[~p & 1], *ro = row[~p & 1];
-        // where each digit's tokens begin: the totals of all rounds
-        for (int d = threadIdx.x; d <= int(mask); d += kSortBlock) first[d] = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kSortBlock) atomicAdd(&first[k[i] >> p * bits & mask], 1u);
-        __syncthreads();
-        exclusive_sum(first, int(mask) + 1);
-        for (int i0 = 0; i0 < n; i0 += kSortBlock) {
-            const int i = i0 + threadIdx.x;
-            const bool live = i < n;
-            clear_counts(counts);
-            const uint32_t x = live ? k[i] : 0, d = x >> p * bits & mask;
-            const uint32_t rank = rank_in_block(d, bits, live, counts, totals);
-            if (live) {
-                ko[first[d] + rank] = x;
-                ro[first[d] + rank] = r[i];
+    const int lane = threadIdx.x % kWave;
+    const int i0 = blockIdx.x * kRankTokens + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kRankEach;
+    if (i0 >= n) return;
+    uint32_t mine[kRankEach], place[kRankEach] = {};
+#pragma unroll
+    for (int t = 0; t < kRankEach; ++t) mine[t] = __builtin_amdgcn_readfirstlane(int(key[i0 + t < n ? i0 + t : n - 1]));
+    // (the two tokens lie in one chunk: equal keys count in the chunks before it, not in those after)
+    const int home = i0 / kChunk;
+    for (int c = 0; c < chunks; ++c) {
+        const uint4 k4 = *reinterpret_cast<const uint4*>(key + c * kChunk + lane * 4);
+        const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+        if (c == home) {
+#pragma unroll
+            for (int t = 0; t < kRankEach; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    place[t] += __popcll(__ballot(k[e] < mine[t] + (c * kChunk + lane * 4 + e < i0 + t ? 1 : 0)));
+        } else {
+#pragma unroll
+            for (int t = 0; t < kRankEach; ++t) {
+                const uint32_t below = mine[t] + (c < home ? 1 : 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) place[t] += __popcll(__ballot(k[e] < below));
             }
-            __syncthreads();
-            for (int j = threadIdx.x; j <= int(mask); j += kSortBlock) first[j] += totals[j];
-            __syncthreads();
         }
     }
-    for (int i = threadIdx.x; i < n; i += kSortBlock) {
-        keys[i] = key[passes & 1][i];
-        rows[i] = row[passes & 1][i];
-    }
+#pragma unroll
+    for (int t = 0; t < kRankEach; ++t)
+        if (lane == t && i0 + t < n) {
+            keys[place[t]] = mine[t];
+            rows[place[t]] = i0 + t;
+        }
 }
 
 // Tokens of each value of a digit in each tile: counts [tiles, digits].  FIRST: the keys are the
@@ -464,7 +469,7 @@ int64_t embed_grad_threads(int64_t n, int64_t V, int64_t D)
     const EmbedGradPlan p = embed_grad_plan(n, V, D);
     const int64_t columns = kSumBlock * (D < 4 ? 1 : 4);
     const int64_t sum = p.windows * ((D + columns - 1) / columns) * kSumBlock * kJoinParts;
-    const int64_t sort = (p.tiles + 1 + kFillBlocks) * kSortBlock;
+    const int64_t sort = (p.tiles + kSmall / kRankTokens + kFillBlocks) * kSortBlock;
     return sum > sort ? sum : sort;
 }
 
@@ -495,8 +500,8 @@ hipError_t launch_embed_grad(const void* dy, const int32_t* ids, int64_t n, int6
     if (p.tiles == 0) {
         const Zeros z = share();
         if (n == 0 && z.count == 0) return hipSuccess;
-        hipLaunchKernelGGL(sort_small_kernel, grid(1, z), block, 0, stream, ids, int(n), uint32_t(V), p.passes, p.bits,
-                           keys[0], rows[0], z);
+        hipLaunchKernelGGL(rank_kernel, grid((n + kRankTokens - 1) / kRankTokens, z), block, 0, stream, ids, int(n),
+                           uint32_t(V), keys[0], rows[0], z);
         if ((e = hipGetLastError()) != hipSuccess || n == 0) return e;
     } else {
         uint32_t* counts = reinterpret_cast<uint32_t*>(ws + p.off_counts);
