@@ -1,11 +1,11 @@
 // Gradient of the embedding's table: dW[v] = scale sum over the tokens k of id v of dy[k].
 //
 // The tokens are sorted by id (a stable counting sort, digit by digit, from the least; few
-// tokens by counting for each what comes before it), so that a row's tokens lie side by side in the order of their positions and their sum has the
-// same bits on every call.  Then a workgroup takes a window of sorted tokens and walks it with
-// its columns in registers: what begins and ends in the window is stored, what crosses a
-// border goes to the workspace (at most one run enters and one leaves a window), and a last
-// launch adds those, window by window.
+// tokens by counting for each what comes before it), so that a row's tokens lie side by side in
+// the order of their positions and their sum has the same bits on every call.  Then a workgroup
+// takes a window of sorted tokens and walks it with its columns in registers: what begins and
+// ends in the window is stored, what crosses a border goes to the workspace (at most one run
+// enters and one leaves a window), and a last launch adds those, window by window.
 //
 // Rows without a token are zeros.  The sort's launches are short and leave the GPU idle, so each
 // has further workgroups that store their share of zeros to all of dW; rows with tokens
