@@ -664,7 +664,8 @@ size_t lh_gated_workspace_bytes(int64_t B, int64_t T, int64_t D);
  *               LH_GATED_MARK, 2 LH_GATED_MARK, ..., which the gradient takes; not written
  *               where a row has no such token; NULL where not needed
  *   workspace : lh_gated_workspace_bytes bytes, 256-byte aligned (NULL allowed when that
- *               is 0)
+ *               is 0), of one call at a time: calls that may run at once, graphs among them,
+ *               need one each
  * Every ld must be less than 2^26 here and in the gradient (not in a step).
  * One kernel launch, or two where the prompt is cut into chunks.
  */

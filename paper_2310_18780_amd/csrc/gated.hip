@@ -95,12 +95,16 @@ __global__ __launch_bounds__(256) void links_kernel(Links links, int64_t words, 
 // The state before block k > 0: from the nearest block before it that leaves one, and those
 // between, each by the decays after it, always in the same order.  Blocks are taken in their order
 // and a workgroup finishes one before it begins the next that it has taken, so the first unfinished
-// block of a tile is always at work and has none to wait for: every wait ends.
+// block of a tile is always at work and has none to wait for: every wait ends.  (Where another
+// call writes the same workspace at the same time, which no call may, it ends all the same, after
+// kPatience looks of half a microsecond or more, and the state is NaN.)
+constexpr int kPatience = 1 << 18;
 __device__ __forceinline__ float look_back(const uint64_t* words, int64_t k, int64_t D)
 {
     constexpr int kLook = 4;  // words loaded together
     const int64_t from = k < kGroup ? 0 : k / kGroup * kGroup - 1;
     float h = 0.f, decay = 0.f;
+    int looks = 0;
     for (int64_t j = k - 1; j >= from;) {
         uint64_t w[kLook];
 #pragma unroll
@@ -116,7 +120,10 @@ __device__ __forceinline__ float look_back(const uint64_t* words, int64_t k, int
                 --j;
             }
         }
-        if (wait) __builtin_amdgcn_s_sleep(1);
+        if (wait) {
+            if (++looks > kPatience) return __builtin_nanf("");
+            __builtin_amdgcn_s_sleep(1);
+        }
     }
     return h;
 }

@@ -79,9 +79,10 @@ def check_gradient(dy, ids, V, scale, dW0=None):
     return dW
 
 
-# (tokens, rows, columns): one workgroup's sort and several's (more than 4096), windows of 16 and of 64 (more than 8192),
-# one to three digits
+# (tokens, rows, columns): placed by counting, or by a sort of one to three digits (more than 8192, where windows are of 64
+# tokens and not of 16)
 SIZES = [(1, 1, 1), (1, 1000, 5), (2, 3, 8), (16, 4, 70), (17, 2, 3), (300, 40, 130), (4096, 300, 9), (4097, 300, 9), (5000, 7, 33),
+         (8191, 4000, 6), (8192, 300, 9), (8193, 300, 9),
          (9000, 5000, 20), (20000, 70000, 4), (12345, 300000, 2), (70000, 513, 5), (3000, 2, 600)]
 
 
