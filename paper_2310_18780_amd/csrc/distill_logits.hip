@@ -8,7 +8,10 @@
 // exponential a value for each.  A workgroup of 4 or 16 wavefronts holds its row in registers
 // as it lies in memory, so that the largest value is known before the exponentials and they are
 // formed again for the gradient without a second read; rows that no workgroup holds are
-// read once more for each.
+// read once more for each.  8192 rows of 50000 bfloat16 with 64 slots, loss and gradient, 15% of
+// them without a loss: 292 us, 1.51 GB at a copy's rate (vector issue 0.58 of the time beside it).
+// With values expanded in registers, a row to a CU, it took 604.  517 x 32003 float32: loss 17 us,
+// gradient 20 (66 and 132 MB, the second read from the cache in part).
 //
 // The slots lie in LDS.  The dense gradient is stored first; then each slot's thread stores its
 // own value over it, all slots of that id subtracted in their order (an id given twice has the

@@ -15,6 +15,10 @@
 // chunk's (log2 A, G), X before it being A X after it + G; each chunk of the second folds
 // those after it.  A chunk's sums over its tokens are one partial row; a last launch adds those
 // in a fixed order.
+//
+// Bound by vector issue (0.59 of the time) beside memory: 4 x 4096 x 2048 bfloat16 with gate
+// takes 45 us for the ends of the chunks and 127 for the gradients (0.64 GB: 124 at a copy's
+// rate).  A first form, which formed the states again from their inputs, took 614.
 #include "gated_ops.hpp"
 
 namespace lh {
@@ -237,6 +241,7 @@ GatedPlan gated_grad_plan(int64_t B, int64_t T, int64_t D)
     // more, and not above five chunks to a step of theirs (prompt and gradient, bfloat16 with gate:
     // 2 x 584 x 128 takes 45 us with chunks of 64 and 31 with 16; 1 x 65536 x 128 takes 150 us
     // with chunks of 120 and 337 with 24)
+    // (6144: the wavefronts that the GPU holds, 6 to a SIMD)
     int64_t least = 16;
     while (least * least * 5 < T) least += kRun;
     GatedPlan p = gated_chunks(B, T, D, 6144, least);
