@@ -8,9 +8,9 @@
 // to a lane, and takes a block of 128 steps, 8 to a wavefront.  Each wavefront forms (A, H) of its
 // run, they meet in LDS, each chains those before its own to its entry state and walks its
 // steps again from registers: inputs are read once, outputs written once.  Where there are
-// rows enough a workgroup goes from block to block; else each block has a workgroup, which
-// leaves what its block alone does to a state as soon as it knows that, and finds the state
-// before it by looking back at the blocks before.
+// rows enough a workgroup goes from block to block; else several take a tile's blocks in turn, and
+// each leaves what its block alone does to a state as soon as it knows that, and finds the
+// state before it by looking back at the blocks before.
 //
 // Bound by vector issue beside memory: a step of a channel is 36 vector instructions and 8
 // transcendental ones, about 275 cycles of a wavefront.  16 x 4096 x 2048 bfloat16 with gate:

@@ -74,7 +74,8 @@ def ref_args(c):
 
 
 SHAPES = [(1, 1, 1), (1, 2, 3), (2, 7, 64), (3, 64, 65), (2, 65, 70), (1, 127, 130), (1, 128, 64), (2, 129, 67), (1, 700, 100),
-          (5, 300, 33), (400, 3, 64), (2, 1025, 5), (390, 140, 10)]
+          (5, 300, 33), (400, 3, 64), (2, 1025, 5), (390, 140, 10),
+          (1, 256, 64), (1, 257, 64), (1, 2200, 3), (159, 390, 7), (160, 390, 7)]
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
