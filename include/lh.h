@@ -762,7 +762,9 @@ lh_status lh_distill_logits(const void* logits, int64_t ld_logits, const float* 
                             size_t workspace_bytes, void* stream);
 
 /* The gradient for an upstream gradient dloss [rows] (float32) of the losses: dlogits of
- * lh_distill_logits times dloss, from its lse.  One kernel launch; no workspace. */
+ * lh_distill_logits times dloss, from its lse.  Where |lse| > 16 its rounding would count
+ * for more than that of the exponentials: there the row's sum is formed again, and lse only
+ * says so.  One kernel launch; no workspace. */
 lh_status lh_distill_logits_backward(const float* dloss, const void* logits, int64_t ld_logits,
                                      const float* values, const int32_t* ids, const float* scale,
                                      const float* lse, int64_t rows, int64_t V, int64_t K,
