@@ -178,7 +178,9 @@ __global__ __launch_bounds__(kBlock) void verify_pick_kernel(Rows<T> a, const do
                 const double y = __shfl_up(c, o, kWave);
                 if (lane >= o) c += y;
             }
-            const uint64_t past = __ballot(before + c > border), any = __ballot(x > 0.);
+            // (only a tile with weight: the lanes' sums are added in different orders, so that one without
+            // may be a rounding past the sum before it, and the border lie between)
+            const uint64_t past = __ballot(x > 0. && before + c > border), any = __ballot(x > 0.);
             if (any) {
                 const int l = kWave - 1 - __builtin_clzll(any);
                 some = i0 + l;
