@@ -636,7 +636,8 @@ lh_status lh_selective_backward(const lh_selective_inputs* in, const lh_selectiv
  *   y = h,  times z sigmoid(z) where z is given
  *
  * rate >= 0 and finite: how fast a channel can forget (0: it holds its state; below 0 the
- * results are NaN).
+ * results are NaN).  A gate below 2^-126 (x below about -87.3) is 0.  A state that is not finite
+ * stays so (where tokens follow an infinity, it may be NaN).
  */
 typedef struct lh_gated_inputs {
     const float* rate;      /* [D] */

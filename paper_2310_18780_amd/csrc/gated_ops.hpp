@@ -172,12 +172,14 @@ __device__ __forceinline__ GateStep gate_step(float r, float i, float u, bool th
     return g;
 }
 
-// A gate's sigmoid(x) from y = -x log2 e, and 1 - sigmoid(x), both without cancellation.
+// A gate's sigmoid(x) from y = -x log2 e, and 1 - sigmoid(x), both without cancellation.  From e =
+// 2^126 on the reciprocal is below the smallest normal number, and is 0: so are then all gradients
+// through the gate, and of e just this limit keeps infinity times 0 away.
 __device__ __forceinline__ float2 gate_pair(float y)
 {
     const float e = exp2_fast(y);
     const float f = rcp_fast(1.f + e);
-    return make_float2(f, fminf(e, 0x1p125f) * f);  // (infinity times 0 would be NaN)
+    return make_float2(f, fminf(e, 0x1p126f) * f);
 }
 
 }  // namespace lh
