@@ -744,12 +744,14 @@ size_t lh_distill_logits_workspace_bytes(int64_t rows, int64_t V, int64_t K);
  *
  * (an id given twice counts twice).  A row without such a slot, or whose scale is 0, has
  * loss and gradient 0 and its logits are not read (the memory must be accessible all the
- * same); its lse is 0.  A row whose logits are all -infinity has q = 0.
+ * same); its lse is 0.  A row whose logits are all -infinity has q = 0.  The sums are float32,
+ * and the loss is a difference of logarithms: it is off by some 2^-20 scale tau^2, which is
+ * much of it where tau is large and p near q.
  *
  *   logits  : [rows, V] (io_dtype), rows ld_logits apart
  *   values  : [rows, K] float32;  ids : [rows, K] int32
  *   scale   : [rows] float32, or NULL (1)
- *   rows >= 0, V >= 1, 1 <= K <= LH_DISTILL_MAX_TOP, tau > 0 and finite; V < 2^31
+ *   rows >= 0, V >= 1, 1 <= K <= LH_DISTILL_MAX_TOP, 2^-60 <= tau <= 2^60; V < 2^31
  *   loss    : out [rows] float32
  *   lse     : out [rows] float32, which lh_distill_logits_backward takes; or NULL
  *   dlogits : out [rows, V] (io_dtype), rows ld_dlogits apart, the gradient of the sum of

@@ -8,8 +8,6 @@
 #include "lh_internal.hpp"
 #include "verify.hpp"
 
-#include <math.h>
-
 using namespace lh::check;
 
 namespace {
@@ -128,8 +126,9 @@ lh_status check_distill(const void* logits, int64_t ld, const float* values, con
     if ((s = check_distill_sizes(rows, V, K)) || (s = check_dtype(io_dtype)) ||
         (s = check_ld("ld_logits", ld, V, rows)) || (dlogits && (s = check_ld("ld_dlogits", ld_d, V, rows))))
         return s;
-    if (!(tau > 0.f) || !isfinite(tau))
-        return fail(LH_ERR_INVALID_ARG, "tau = %g must be > 0 and finite", double(tau));
+    // (its square and its reciprocal are normal numbers)
+    if (!(tau >= 0x1p-60f && tau <= 0x1p60f))
+        return fail(LH_ERR_INVALID_ARG, "tau = %g must be in [2^-60, 2^60]", double(tau));
     if (rows > 0 && (!logits || !values || !ids))
         return fail(LH_ERR_INVALID_ARG, "logits, values and ids must not be NULL");
     const size_t es = esize(io_dtype);
