@@ -668,7 +668,7 @@ size_t lh_gated_workspace_bytes(int64_t B, int64_t T, int64_t D);
  *               is 0), of one call at a time: calls that may run at once, graphs among them,
  *               need one each
  * Every ld must be less than 2^26 here and in the gradient (not in a step).
- * One kernel launch, or two where the prompt is cut into chunks.
+ * One kernel launch, or two where rows are few and workgroups share a prompt's blocks.
  */
 lh_status lh_gated_prefill(const lh_gated_inputs* in, int resume, float* state, void* y,
                            float* marks, void* workspace, size_t workspace_bytes, void* stream);

@@ -204,7 +204,7 @@ __global__ __launch_bounds__(kWaves* kWave, 8) void gated_kernel(GatedIn<T> in, 
         const bool last = k == blocks - 1;
         if constexpr (CHAIN) {
             if (wave == kWaves - 1) {
-                uint64_t* words = links.words + at.b * in.chunks * in.D + c;
+                uint64_t* words = links.words + at.b * in.blocks * in.D + c;
                 const bool leaves = k == 0 || k % kGroup == kGroup - 1;
                 if (!last && !leaves) post(words + k * in.D, hend, lend);
                 if (k > 0) h = look_back(words, k, in.D);
@@ -279,23 +279,23 @@ hipError_t gated(const Gated& g, float* state, bool resume, T* y, float* marks, 
                  hipStream_t stream)
 {
     const GatedPlan p = gated_plan(g.B, g.T, g.D);
-    const GatedIn<T> in = gated_in<T>(g, p);
+    const GatedIn<T> in = gated_in<T>(g, g.T > 0 ? g.T : 1, 1, p.blocks);
     const int64_t tiles = g.B * in.tiles;
     const dim3 block(kWaves * kWave);
     Links links{};
-    if (p.ws_bytes == 0) {
+    if (p.shares == 1) {
         hipLaunchKernelGGL((gated_kernel<T, GATE, false>), dim3(uint32_t(tiles)), block, 0, stream, in, state,
                            int(resume), y, marks, links);
         return hipGetLastError();
     }
-    const int64_t words = g.B * p.chunks * g.D, fills = (words + 1023) / 1024;
+    const int64_t words = g.B * p.blocks * g.D, fills = (words + 1023) / 1024;
     links.words = static_cast<uint64_t*>(workspace);
     links.tickets = reinterpret_cast<uint32_t*>(links.words + words);
     hipLaunchKernelGGL(links_kernel, dim3(uint32_t(fills < 1024 ? fills : 1024)), dim3(256), 0, stream, links, words,
                        tiles);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL((gated_kernel<T, GATE, true>), dim3(uint32_t(tiles * gated_shares(tiles, p.chunks))), block, 0,
-                       stream, in, state, int(resume), y, marks, links);
+    hipLaunchKernelGGL((gated_kernel<T, GATE, true>), dim3(uint32_t(tiles * p.shares)), block, 0, stream, in,
+                       state, int(resume), y, marks, links);
     return hipGetLastError();
 }
 
@@ -303,18 +303,17 @@ hipError_t gated(const Gated& g, float* state, bool resume, T* y, float* marks, 
 
 GatedPlan gated_plan(int64_t B, int64_t T, int64_t D)
 {
-    // (every workgroup sees the whole prompt)
-    GatedPlan p{T > 0 ? T : 1, T > 0 ? (T + kSpan - 1) / kSpan : 1, 0};
+    GatedPlan p{T > 0 ? (T + kSpan - 1) / kSpan : 1, 1, 0};
     const int64_t tiles = gated_tiles(B, D);
-    if (gated_shares(tiles, p.chunks) > 1)
-        p.ws_bytes = (sizeof(uint64_t) * size_t(B) * p.chunks * D + sizeof(uint32_t) * size_t(tiles) + 7) / 8 * 8;
+    p.shares = gated_shares(tiles, p.blocks);
+    if (p.shares > 1)
+        p.ws_bytes = (sizeof(uint64_t) * size_t(B) * p.blocks * D + sizeof(uint32_t) * size_t(tiles) + 7) / 8 * 8;
     return p;
 }
 
 int64_t gated_threads(int64_t B, int64_t T, int64_t D)
 {
-    const int64_t tiles = gated_tiles(B, D);
-    return tiles * gated_shares(tiles, gated_plan(B, T, D).chunks) * kWaves * kWave;
+    return gated_tiles(B, D) * gated_plan(B, T, D).shares * kWaves * kWave;
 }
 
 int64_t gated_step_threads(int64_t B, int64_t D) { return B * ((D + 255) / 256) * 256; }
@@ -331,13 +330,12 @@ hipError_t launch_gated(const Gated& g, float* state, bool resume, void* y, floa
 
 hipError_t launch_gated_step(const Gated& g, float* state, void* y_t, hipStream_t stream)
 {
-    const GatedPlan p{1, 1, 0};
     const dim3 grid(uint32_t(gated_step_threads(g.B, g.D) / 256));
     if (g.bf16_io)
-        hipLaunchKernelGGL((gated_step_kernel<bf16>), grid, dim3(256), 0, stream, gated_in<bf16>(g, p),
+        hipLaunchKernelGGL((gated_step_kernel<bf16>), grid, dim3(256), 0, stream, gated_in<bf16>(g, 1, 1, 1),
                            state, static_cast<bf16*>(y_t));
     else
-        hipLaunchKernelGGL((gated_step_kernel<float>), grid, dim3(256), 0, stream, gated_in<float>(g, p),
+        hipLaunchKernelGGL((gated_step_kernel<float>), grid, dim3(256), 0, stream, gated_in<float>(g, 1, 1, 1),
                            state, static_cast<float*>(y_t));
     return hipGetLastError();
 }

@@ -22,13 +22,19 @@ struct GatedGrads {
     float *drate, *dr_bias, *di_bias, *dfirst;
 };
 
-// Time chunks that a prompt is cut into (chunk: steps of one).
+// A prompt's blocks of steps, and how many workgroups share those of a tile of channels.
 struct GatedPlan {
-    int64_t chunk, chunks;
+    int64_t blocks, shares;
     size_t ws_bytes;
 };
 GatedPlan gated_plan(int64_t B, int64_t T, int64_t D);
-GatedPlan gated_grad_plan(int64_t B, int64_t T, int64_t D);
+
+// Time chunks that the gradient's prompt is cut into (chunk: steps of one).
+struct GatedGradPlan {
+    int64_t chunk, chunks;
+    size_t ws_bytes;
+};
+GatedGradPlan gated_grad_plan(int64_t B, int64_t T, int64_t D);
 
 // Threads of the largest launch of a call.
 int64_t gated_threads(int64_t B, int64_t T, int64_t D);

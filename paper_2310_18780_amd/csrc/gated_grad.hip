@@ -209,8 +209,8 @@ __global__ __launch_bounds__(kWaves* kWave, 6) void gated_grad_kernel(GatedIn<T>
 template <typename T, bool GATE>
 hipError_t gated_grad(const Gated& g, const GatedGrads& d, void* workspace, hipStream_t stream)
 {
-    const GatedPlan p = gated_grad_plan(g.B, g.T, g.D);
-    const GatedIn<T> in = gated_in<T>(g, p);
+    const GatedGradPlan p = gated_grad_plan(g.B, g.T, g.D);
+    const GatedIn<T> in = gated_in<T>(g, p.chunk, p.chunks, 0);
     const int64_t P = g.B * p.chunks, tiles = gated_tiles(g.B, g.D);
     float* part = static_cast<float*>(workspace);
     // (an even number of floats before it, so that pairs are aligned)
@@ -235,7 +235,7 @@ hipError_t gated_grad(const Gated& g, const GatedGrads& d, void* workspace, hipS
 
 }  // namespace
 
-GatedPlan gated_grad_plan(int64_t B, int64_t T, int64_t D)
+GatedGradPlan gated_grad_plan(int64_t B, int64_t T, int64_t D)
 {
     // More chunks fill the GPU where channels are few, but each folds all after it: 16 steps or
     // more, and not above five chunks to a step of theirs (prompt and gradient, bfloat16 with gate:
@@ -244,7 +244,7 @@ GatedPlan gated_grad_plan(int64_t B, int64_t T, int64_t D)
     // (6144: the wavefronts that the GPU holds, 6 to a SIMD)
     int64_t least = 16;
     while (least * least * 5 < T) least += kRun;
-    GatedPlan p = gated_chunks(B, T, D, 6144, least);
+    GatedGradPlan p = gated_chunks(B, T, D, 6144, least);
     const size_t rows = size_t(B) * p.chunks * D;
     p.ws_bytes = sizeof(float) * ((rows * 3 + 1) / 2 * 2) + (p.chunks > 1 ? sizeof(float2) * rows : 0);
     return p;

@@ -10,25 +10,26 @@ namespace lh {
 constexpr int kRun = LH_GATED_MARK;  // steps that a wavefront takes at a time
 constexpr int kTile = kWave;         // channels of a wavefront, one to a lane
 
-// A call's inputs in the types of its kernels.
+// A call's inputs in the types of its kernels.  (The prompt and the step see all their tokens as one
+// chunk.)
 template <typename T>
 struct GatedIn {
     const T *r, *i, *u, *z;
     int64_t ld_r, ld_i, ld_u, ld_z;
     const float *rate, *r_bias, *i_bias;
     const int* lengths;
-    int64_t B, T_, D, chunk, chunks, tiles, marks;
+    int64_t B, T_, D, chunk, chunks, blocks, tiles, marks;
 };
 
 template <typename T>
-GatedIn<T> gated_in(const Gated& g, const GatedPlan& p)
+GatedIn<T> gated_in(const Gated& g, int64_t chunk, int64_t chunks, int64_t blocks)
 {
     GatedIn<T> a;
     a.r = static_cast<const T*>(g.r), a.i = static_cast<const T*>(g.i);
     a.u = static_cast<const T*>(g.u), a.z = static_cast<const T*>(g.z);
     a.ld_r = g.ld_r, a.ld_i = g.ld_i, a.ld_u = g.ld_u, a.ld_z = g.ld_z;
     a.rate = g.rate, a.r_bias = g.r_bias, a.i_bias = g.i_bias, a.lengths = g.lengths;
-    a.B = g.B, a.T_ = g.T, a.D = g.D, a.chunk = p.chunk, a.chunks = p.chunks;
+    a.B = g.B, a.T_ = g.T, a.D = g.D, a.chunk = chunk, a.chunks = chunks, a.blocks = blocks;
     a.tiles = (g.D + kTile - 1) / kTile;
     a.marks = (g.T + kRun - 1) / kRun;
     return a;
@@ -37,12 +38,12 @@ GatedIn<T> gated_in(const Gated& g, const GatedPlan& p)
 inline int64_t gated_tiles(int64_t B, int64_t D) { return B * ((D + kTile - 1) / kTile); }
 
 // Chunks of whole runs for about `want` of them over all tiles, each of `least` steps or more.
-inline GatedPlan gated_chunks(int64_t B, int64_t T, int64_t D, int64_t want, int64_t least)
+inline GatedGradPlan gated_chunks(int64_t B, int64_t T, int64_t D, int64_t want, int64_t least)
 {
     int64_t chunks = want / gated_tiles(B, D);
     if (chunks > T / least) chunks = T / least;
     if (chunks < 1) chunks = 1;
-    GatedPlan p{};
+    GatedGradPlan p{};
     const int64_t runs = (T + kRun - 1) / kRun, per = (runs + chunks - 1) / chunks;
     p.chunk = (per > 0 ? per : 1) * kRun;
     p.chunks = T > 0 ? (T + p.chunk - 1) / p.chunk : 1;
