@@ -711,7 +711,9 @@ lh_status lh_gated_backward(const lh_gated_inputs* in, const lh_gated_grads* gra
 lh_status lh_embed(const void* W, const int32_t* ids, int64_t n, int64_t V, int64_t D,
                    lh_dtype table_dtype, lh_dtype io_dtype, float scale, void* y, void* stream);
 
-/* Workspace bytes of lh_embed_backward (16 n and up to n D / 2); (size_t)-1 for invalid sizes. */
+/* Workspace bytes of lh_embed_backward; (size_t)-1 for invalid sizes.  Each array in it begins
+ * on a border of 256 bytes: four of 4 n bytes; above 8192 tokens the counts of the sort, up
+ * to 256 KiB; and 8 D bytes for each 16 tokens or part of them (64, above 8192 tokens). */
 size_t lh_embed_backward_workspace_bytes(int64_t n, int64_t V, int64_t D);
 
 /*
@@ -721,7 +723,8 @@ size_t lh_embed_backward_workspace_bytes(int64_t n, int64_t V, int64_t D);
  *   dy         : [n, D] (io_dtype);  dW : out [V, D] float32
  *   accumulate : dW is added to (rows without a token are not touched); else every row is
  *                written
- * Ids outside [0, V) take no part.  workspace as in lh_gated_prefill.
+ * Ids outside [0, V) take no part.  workspace as in lh_gated_prefill.  A launch holds fewer
+ * than 2^32 threads: n is below 2^28 for D <= 1024, below 2^27 for D <= 2048, and so on.
  */
 lh_status lh_embed_backward(const void* dy, const int32_t* ids, int64_t n, int64_t V, int64_t D,
                             lh_dtype io_dtype, float scale, int accumulate, float* dW,
@@ -730,7 +733,7 @@ lh_status lh_embed_backward(const void* dy, const int32_t* ids, int64_t n, int64
 /* Largest number of a teacher's logits per row. */
 #define LH_DISTILL_MAX_TOP 1024
 
-/* Workspace bytes of lh_distill_logits; (size_t)-1 for invalid sizes. */
+/* Workspace bytes of lh_distill_logits, at present 0; (size_t)-1 for invalid sizes. */
 size_t lh_distill_logits_workspace_bytes(int64_t rows, int64_t V, int64_t K);
 
 /*
@@ -757,6 +760,7 @@ size_t lh_distill_logits_workspace_bytes(int64_t rows, int64_t V, int64_t K);
  *   dlogits : out [rows, V] (io_dtype), rows ld_dlogits apart, the gradient of the sum of
  *             the losses; or NULL.  It may be the buffer of logits (with the same ld).
  *   workspace as in lh_gated_prefill
+ * One kernel launch.
  */
 lh_status lh_distill_logits(const void* logits, int64_t ld_logits, const float* values,
                             const int32_t* ids, const float* scale, int64_t rows, int64_t V,

@@ -275,9 +275,7 @@ hipError_t distill(const DistillLogits& d, float* loss, float* lse, const float*
 
 }  // namespace
 
-size_t distill_logits_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
-
-hipError_t launch_distill_logits(const DistillLogits& a, float* loss, float* lse, void*, hipStream_t stream)
+hipError_t launch_distill_logits(const DistillLogits& a, float* loss, float* lse, hipStream_t stream)
 {
     if (a.bf16_io)
         return a.dlogits ? distill<bf16, 1>(a, loss, lse, nullptr, stream) : distill<bf16, 0>(a, loss, lse, nullptr, stream);

@@ -19,9 +19,7 @@ struct DistillLogits {
     int64_t ld_d;
 };
 
-size_t distill_logits_workspace_bytes(int64_t rows, int64_t V, int64_t K);
-hipError_t launch_distill_logits(const DistillLogits& a, float* loss, float* lse, void* workspace,
-                                 hipStream_t stream);
+hipError_t launch_distill_logits(const DistillLogits& a, float* loss, float* lse, hipStream_t stream);
 hipError_t launch_distill_logits_grad(const DistillLogits& a, const float* dloss, const float* lse,
                                       hipStream_t stream);
 
