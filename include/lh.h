@@ -723,7 +723,8 @@ size_t lh_embed_backward_workspace_bytes(int64_t n, int64_t V, int64_t D);
  *   dy         : [n, D] (io_dtype);  dW : out [V, D] float32
  *   accumulate : dW is added to (rows without a token are not touched); else every row is
  *                written
- * Ids outside [0, V) take no part.  workspace as in lh_gated_prefill.  A launch holds fewer
+ * Ids outside [0, V) take no part.  The same inputs give the same bits; other tokens beside a
+ * row's may group its sum otherwise.  workspace as in lh_gated_prefill.  A launch holds fewer
  * than 2^32 threads: n is below 2^28 for D <= 1024, below 2^27 for D <= 2048, and so on.
  */
 lh_status lh_embed_backward(const void* dy, const int32_t* ids, int64_t n, int64_t V, int64_t D,

@@ -244,13 +244,15 @@ hipError_t with_shape(int64_t V, int K, F f)
         const int64_t n = (pieces + B - 1) / B;
         if (n <= 1) return f(block, std::integral_constant<int, 1>());
         if (n <= 2) return f(block, std::integral_constant<int, 2>());
-        if (n <= 4) return f(block, std::integral_constant<int, 4>());
-        if constexpr (B == 1024) {
+        if constexpr (B < 1024) {  // (four at most)
+            return f(block, std::integral_constant<int, 4>());
+        } else {
+            if (n <= 4) return f(block, std::integral_constant<int, 4>());
             if (n <= 6) return f(block, std::integral_constant<int, 6>());
             if (n <= 8) return f(block, std::integral_constant<int, 8>());
             if (n <= kHold) return f(block, std::integral_constant<int, kHold>());
+            return f(block, std::integral_constant<int, 0>());
         }
-        return f(block, std::integral_constant<int, 0>());
     };
     if (pieces <= 4 * 256 && K <= 256) return iters(std::integral_constant<int, 256>());
     return iters(std::integral_constant<int, 1024>());

@@ -439,9 +439,10 @@ hipError_t launch_runs(const T* dy, const uint32_t* keys, const uint32_t* rows, 
 EmbedGradPlan embed_grad_plan(int64_t n, int64_t V, int64_t D)
 {
     EmbedGradPlan p{};
-    // 64 tokens, one to a lane, where that gives windows enough for every CU; of few tokens 16, so
-    // that more workgroups share them (65536 tokens x 2048: runs and joins 124 + 13 us with windows
-    // of 64, 120 + 27 with 32, 120 + 46 with 16)
+    // 64 tokens, one to a lane; of few tokens 16, so that more workgroups share them.  The number of
+    // tokens alone decides: 8193 to 16384 of them, up to 1024 columns wide, are fewer workgroups than
+    // CUs.  (65536 tokens x 2048: runs and joins 124 + 13 us with windows of 64, 120 + 27 with 32,
+    // 120 + 46 with 16)
     p.window = n <= 8192 ? 16 : kWave;
     p.windows = (n + p.window - 1) / p.window;
     int bits = 1;  // of the keys 0 .. V
